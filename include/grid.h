@@ -546,6 +546,7 @@ size_t grid_forced_span_workspace_bytes(const grid_compiled* g, int32_t B);
 /* -------------------------------------------------------------------- apply */
 #define GRID_DTYPE_F32 0
 #define GRID_DTYPE_BF16 1
+#define GRID_DTYPE_F16 2   /* grid_kv_append, grid_attend and grid_verify only */
 /* In place: logits[b * row_stride + t] = -inf for every t < V whose mask bit
  * is 0 (fp32 0xFF800000, bf16 0xFF80); other entries keep their bit patterns
  * (section 2: hard -inf masking, a soundness precondition of Proposition 7).
@@ -557,6 +558,163 @@ size_t grid_forced_span_workspace_bytes(const grid_compiled* g, int32_t B);
  * Asynchronous on stream. */
 int grid_apply(const uint32_t* mask_dev, void* logits_dev, int32_t dtype, int32_t B, int32_t V,
                int64_t row_stride, void* stream);
+
+/* ------------------------------------------------------------- paged cache */
+/* The model's side of a decoding step.  A sequence's chunk of new tokens (a
+ * sampled token, a forced span, drafted tokens, a prompt) is appended to a
+ * paged key / value cache (grid_kv_append), attends over it (grid_attend) and,
+ * where the tokens were drafted, is verified under the masks (grid_verify).
+ * These calls need no compiled handle. */
+
+/* A cache in caller-owned device memory: entry (page, row, head, i) of the
+ * keys is k_pages[page * k_stride[0] + row * k_stride[1] + head * k_stride[2]
+ * + i], of the values likewise with v_stride (strides in elements, multiples
+ * of 8, not negative; pages 16-byte aligned).  So a page may hold its rows
+ * before its heads or its heads before its rows. */
+typedef struct {
+  void* k_pages;        /* device, dtype */
+  void* v_pages;        /* device, dtype */
+  int32_t dtype;        /* GRID_DTYPE_BF16 or GRID_DTYPE_F16 */
+  int32_t n_pages;      /* >= 1 */
+  int32_t page_size;    /* rows of a page, 1 .. 65536 */
+  int32_t n_kv_heads;   /* 1 .. 1024 */
+  int32_t head_dim;     /* a multiple of 8, 8 .. 256; grid_attend: 64, 128 or 256 */
+  int64_t k_stride[3];  /* page, row, head */
+  int64_t v_stride[3];
+} grid_paged_cache;
+
+/* The chunks of a batch.  Token t of sequence b, cu_q[b] <= t < cu_q[b + 1],
+ * is the chunk's token i = t - cu_q[b] and has the position
+ * kv_len[b] - (cu_q[b + 1] - cu_q[b]) + i: kv_len counts the sequence's tokens
+ * with the chunk.  Position s of sequence b is row s % page_size of page
+ * block_table[b * table_stride + s / page_size].  A chunk may be empty; tokens
+ * before cu_q[0] and from cu_q[n_seqs] on belong to no sequence.  A sequence
+ * is bad when cu_q[b] < 0, cu_q[b + 1] < cu_q[b], cu_q[b + 1] > n_tokens,
+ * or kv_len[b] is less than the chunk or more than table_cols * page_size; what
+ * a call does with it, and with a page id that is not in 0 .. n_pages - 1, is
+ * said there.  No call leaves the cache's bounds. */
+typedef struct {
+  int32_t n_seqs;              /* B, 1 .. 65535 */
+  int32_t n_tokens;            /* rows of the packed arrays, 0 .. 2^24 */
+  const int32_t* block_table;  /* device [B][table_stride] */
+  int64_t table_stride;        /* >= table_cols */
+  int32_t table_cols;          /* >= 1, table_cols * page_size < 2^31 */
+  const int32_t* kv_len;       /* device [B] */
+  const int32_t* cu_q;         /* device [B + 1] */
+} grid_chunks;
+
+/* Writes the chunk's keys and values into the cache and, with q, the chunk's
+ * queries into q_out.  Keys and queries x (a head's vector of one token) are
+ * first normed where a weight is given, x * rsqrt(mean(x^2) + eps) * weight,
+ * then rotated by the position p where tables are given: of the first rot_dim
+ * entries the pairs (j, j + rot_dim / 2), or with interleaved (2j, 2j + 1),
+ * become (a cos - c sin, c cos + a sin) with cos[p * rot_dim / 2 + j] and sin
+ * alike.  All of it in 32 bits, rounded once to the dtype; without either, and
+ * for the values, entries are copied.  Two tokens must not share a place in the cache. */
+typedef struct {
+  const void* k;           /* device [n_tokens], strides below, the cache's dtype */
+  const void* v;
+  const void* q;           /* or NULL: no queries */
+  void* q_out;             /* may be q (same strides) */
+  int32_t n_heads;         /* query heads (with q) */
+  int64_t k_stride[2];     /* token, head; in elements, multiples of 8; 16-byte aligned */
+  int64_t v_stride[2];
+  int64_t q_stride[2];
+  int64_t q_out_stride[2];
+  const float* cos;        /* device [n_positions][rot_dim / 2], or both NULL */
+  const float* sin;
+  int32_t n_positions;     /* rows of cos and sin */
+  int32_t rot_dim;         /* 2 .. head_dim; a multiple of 16, or with interleaved of 8 */
+  int32_t interleaved;
+  const float* q_norm;     /* device [head_dim], or NULL */
+  const float* k_norm;
+  float eps;               /* >= 0 */
+  int32_t* status;         /* device [n_seqs] or NULL: GRID_ROW_OK, or GRID_ROW_BAD_CONFIG for a bad
+                              sequence and for one with a token whose page is not in the cache or
+                              whose position has no row of cos and sin; such tokens (of a bad sequence
+                              all) are left out, in the cache and in q_out */
+} grid_append_args;
+int grid_kv_append(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_append_args* args, void* stream);
+
+/* Attention of the chunks over the cache, their own entries among it
+ * (grid_kv_append comes first).  Query head h reads key head
+ * h / (n_heads / n_kv_heads).  Token t at position p sees the positions s <= p,
+ * with a window w > 0 those with s > p - w too:
+ *   out[t][h] = sum over s of softmax(scale * q[t][h] . K[s]) V[s],
+ *   lse[t][h] = log of the sum over s of exp(scale * q[t][h] . K[s]).
+ * Scores, softmax and sums are held in 32 bits; the weights are rounded to the
+ * dtype before they multiply V, the result once at the end.  What a token does
+ * not see has no part in its result, infinities and NaN there included.
+ * max_q and max_kv bound the chunks' lengths and kv_len; they fix the launch.
+ * The rows of a sequence that is bad or longer than they say are NaN, and so
+ * are those that would read a page that is not in the cache (others of that
+ * sequence may be).  Rows of tokens that belong to no sequence are left as they
+ * are.
+ * Workspace: device scratch, 16-byte aligned, of at least
+ * grid_attend_workspace_bytes; nothing is expected in it. */
+typedef struct {
+  const void* q;           /* device [n_tokens], the cache's dtype */
+  void* out;
+  int64_t q_stride[2];     /* token, head; in elements, multiples of 8; 16-byte aligned */
+  int64_t out_stride[2];
+  float* lse;              /* device [n_tokens][n_heads] or NULL */
+  int32_t n_heads;         /* a multiple of n_kv_heads, at most 1024 */
+  int32_t max_q;           /* >= 1 */
+  int32_t max_kv;          /* >= 1 */
+  int32_t window;          /* 0: none */
+  float scale;             /* finite */
+  void* workspace;
+  size_t workspace_bytes;
+} grid_attend_args;
+int grid_attend(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_attend_args* args, void* stream);
+/* Of args and chunks only the sizes are read; 0 on bad sizes. */
+size_t grid_attend_workspace_bytes(const grid_paged_cache* cache, const grid_chunks* chunks,
+                                   const grid_attend_args* args);
+
+/* Verification of drafted tokens.  Row (b, j), j <= draft_len[b] <= K, of the
+ * logits is the target's distribution after j drafted tokens of sequence b:
+ * p = softmax(logits / temperature[b]) over the tokens its mask row allows.
+ * Draft x_j is accepted when those before it are and
+ *   uniform[b][j] * q(x_j) < p(x_j)
+ * with q the row of draft_probs, or, without, all of q on x_j.  The next token
+ * comes from row a = the number accepted: the index that makes w / noise[b] the
+ * largest (the lowest such index), w = p where every draft was accepted and
+ * max(p - q, 0) where one was refused (p, if that leaves nothing).  With
+ * noise drawn from Exp(1) and uniform from U[0, 1) the tokens follow the
+ * target's distribution.  A temperature that is not above 0, or no uniform and
+ * no noise, is greedy: p is 1 at the largest logit (the lowest such index).
+ * A row with no distribution (nothing allowed, or an allowed logit that is NaN or
+ * +inf) accepts nothing and gives the token -1.
+ * tokens[b] = the accepted drafts, the next token, then -1; accepted[b] = a;
+ * logprobs[b][j] = log p of tokens[b][j] (greedy: at temperature 1), 0 at -1.
+ * draft_len is clamped to 0 .. K; a drafted id outside 0 .. V - 1 is refused.
+ * Statistics are held in 32 bits. */
+typedef struct {
+  const void* logits;          /* device [B][K + 1][V] */
+  int32_t dtype;               /* GRID_DTYPE_F32, _BF16 or _F16 */
+  int32_t B;                   /* 1 .. 65535 */
+  int32_t K;                   /* 0 .. 63 */
+  int32_t V;                   /* >= 1 */
+  int64_t logits_stride[2];    /* sequence, row; in elements */
+  const uint32_t* mask;        /* device rows of the mask layout, or NULL: all allowed */
+  int64_t mask_stride[2];      /* sequence, row; in words */
+  const int32_t* draft;        /* device [B][K] (K > 0) */
+  const int32_t* draft_len;    /* device [B], or NULL: K */
+  const float* draft_probs;    /* device [B][K][V], or NULL */
+  int64_t probs_stride[2];
+  const float* uniform;        /* device [B][K], or NULL with noise */
+  const float* noise;          /* device [B], rows of V */
+  int64_t noise_stride;
+  const float* temperature;    /* device [B], or NULL: 1 */
+  int32_t* tokens;             /* device [B][K + 1] */
+  int32_t* accepted;           /* device [B] */
+  float* logprobs;             /* device [B][K + 1] */
+  void* workspace;             /* device scratch, 16-byte aligned, grid_verify_workspace_bytes */
+  size_t workspace_bytes;
+} grid_verify_args;
+int grid_verify(const grid_verify_args* args, void* stream);
+/* 0 on bad sizes. */
+size_t grid_verify_workspace_bytes(int32_t B, int32_t K, int32_t V);
 
 #ifdef __cplusplus
 }

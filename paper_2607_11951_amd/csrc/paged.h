@@ -1,0 +1,72 @@
+// paged.h -- the paged cache and the chunks of a batch as the kernels see them.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <string>
+
+#include "host.h"
+
+namespace grid {
+
+int fail(int code, const std::string& msg);
+void clear_error();
+
+typedef __bf16 bf16_t;
+typedef _Float16 f16_t;
+
+// n / d for n < 2^31 as (n * mul) >> shift: with l = ceil(log2 d), mul = floor(2^(31 + l) / d) + 1 exceeds
+// 2^(31 + l) / d by at most 1 = 2^l / 2^l, an error of n / 2^(31 + l) * 2^l / d < 1 / d in the quotient.
+struct Divisor {
+  uint32_t d, mul, shift;
+  explicit Divisor(uint32_t div = 1) : d(div) {
+    uint32_t l = 0;
+    while ((1u << l) < div) ++l;
+    mul = (uint32_t)(((uint64_t)1 << (31 + l)) / div + 1);
+    shift = 31 + l;
+  }
+  __host__ __device__ uint32_t quot(uint32_t n) const { return (uint32_t)(((uint64_t)n * mul) >> shift); }
+};
+
+struct Paged {
+  uint16_t *k, *v;  // both dtypes have 16 bits
+  int64_t ks[3], vs[3];
+  const int32_t* table;
+  int64_t table_stride;
+  const int32_t* kv_len;
+  const int32_t* cu_q;
+  Divisor page;
+  int32_t n_pages, cols, hkv, D, B, T;
+  int64_t reach;  // positions the table has room for
+
+  // page id of position s (0 <= s < reach) of sequence b: may be out of range, see in_cache
+  __device__ int page_of(int b, uint32_t s, uint32_t& row) const {
+    const uint32_t c = page.quot(s);
+    row = s - c * page.d;
+    return table[(int64_t)b * table_stride + c];
+  }
+  __device__ bool in_cache(int id) const { return (uint32_t)id < (uint32_t)n_pages; }
+};
+
+// Checks a cache and chunks; the message names the call.
+int check_paged(const char* call, const grid_paged_cache* c, const grid_chunks* x, bool pointers);
+Paged make_paged(const grid_paged_cache* c, const grid_chunks* x);
+// Whether rows of `head_dim` at these strides (elements of 16 bits) can be read 16 bytes at a time.
+bool rows_fit(const void* p, const int64_t* strides, int n);
+
+struct Chunk {
+  int32_t first, n, kv;  // first token, new tokens, cached tokens with them
+  bool ok;
+};
+__device__ inline Chunk chunk_of(const Paged& P, int b) {
+  Chunk c;
+  c.first = P.cu_q[b];
+  const int32_t end = P.cu_q[b + 1];
+  c.kv = P.kv_len[b];
+  c.ok = c.first >= 0 && end >= c.first && end <= P.T;
+  c.n = c.ok ? end - c.first : 0;
+  c.ok = c.ok && c.kv >= c.n && c.kv <= P.reach;
+  return c;
+}
+
+}  // namespace grid

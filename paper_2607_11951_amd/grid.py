@@ -22,7 +22,7 @@ ERRORS = {
 }
 ROW_OK, ROW_EMPTY, ROW_BAD_CONFIG, ROW_OVERFLOW, ROW_NOT_VIABLE, ROW_FINISHED = 0, 1, 2, 4, 8, 16
 CACHE_LOOKUP, CACHE_INSERT = 1, 2
-DTYPE_F32, DTYPE_BF16 = 0, 1
+DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
 
 ART_NAMES = ["DFA_DENSE", "DFA_CLASS", "BYTE_CLASS", "DFA_ACCEPT_OFF", "DFA_ACCEPT_LIST", "DFA_LIVE",
              "ACTION", "GOTO", "PROD", "TERM_INFO", "SPELL_OFF", "SPELL_BYTES", "ALIAS_OFF",
@@ -47,7 +47,8 @@ EXPORTS = ["grid_compile", "grid_free", "grid_last_error", "grid_info", "grid_ad
            "grid_cache_bytes", "grid_cache_clear", "grid_mask_cached", "grid_accept",
            "grid_mask_noalloc_max_bytes", "grid_mask_noalloc", "grid_stack_hash", "grid_stack_hash_host",
            "grid_accept_inplace", "grid_ci_cache_bytes", "grid_ci_cache_clear", "grid_mask_warm",
-           "grid_complete", "grid_forced_span", "grid_forced_span_workspace_bytes"]
+           "grid_complete", "grid_forced_span", "grid_forced_span_workspace_bytes", "grid_kv_append", "grid_attend",
+           "grid_attend_workspace_bytes", "grid_verify", "grid_verify_workspace_bytes"]
 CI_LOOKUP, CI_INSERT, CI_FAMILY, CI_GENN = 1, 2, 4, 8
 PHASE_PROLOGUE, PHASE_WALK, PHASE_RESIDUE, PHASE_FINALIZE, PHASE_ALL = 1, 2, 4, 8, 15
 
@@ -123,6 +124,13 @@ def lib():
         L.grid_mask_noalloc_max_bytes.argtypes = []
         L.grid_mask_noalloc_max_bytes.restype = sz
         L.grid_mask_noalloc.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp]
+        L.grid_kv_append.argtypes = [vp, vp, vp, vp]
+        L.grid_attend.argtypes = [vp, vp, vp, vp]
+        L.grid_attend_workspace_bytes.argtypes = [vp, vp, vp]
+        L.grid_attend_workspace_bytes.restype = sz
+        L.grid_verify.argtypes = [vp, vp]
+        L.grid_verify_workspace_bytes.argtypes = [i32, i32, i32]
+        L.grid_verify_workspace_bytes.restype = sz
         _lib = L
     return _lib
 

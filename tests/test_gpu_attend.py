@@ -1,0 +1,450 @@
+"""grid_kv_append and grid_attend on the GPU against plain implementations in 64 bits.
+
+Bounds.  Inputs are exact in both; u is half a unit in the last place of the dtype (2^-8 bf16, 2^-11 f16 relative; f16
+below 2^-14 absolute 2^-25).
+ * append: 32-bit arithmetic (relative error below 2^-20 of the operands' size) and one rounding:
+   |y - ref| <= u |ref| + 2^-20 size + 2^-25.
+ * attend: a score is a sum of D products in 32 bits, off by at most e = (D + 8) 2^-24 scale sum |q_i k_i|; a weight
+   then is off by a factor of 1 +- (e + 2^-20) and rounded (u); so is the result, once:
+   |out - ref| <= (u + 2 e + 2^-18) sum p |v| + u |ref| + n 2^-25 max |v|, and |lse - ref| <= e + 2^-20 (1 + |ref|).
+   The f16 term n 2^-25 is what n weights below 2^-14 of the largest lose.
+"""
+
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f16": torch.float16}
+U = {dt: torch.finfo(dt).eps / 2 for dt in DT.values()}
+
+
+@pytest.fixture(scope="module")
+def G():
+    import paper_2607_11951_amd as pkg
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    pkg.lib()
+    return pkg
+
+
+class Batch:
+    """Sequences of (new, cached with them) tokens in pages handed out in random order."""
+
+    def __init__(self, lens, heads, page, dtype, seed=0, heads_first=False, spare=1, extra_cols=0):
+        self.hq, self.hkv, self.D = heads
+        self.lens, self.page, self.dt = lens, page, DT[dtype]
+        self.gen = torch.Generator(device="cuda").manual_seed(seed)
+        rng = np.random.default_rng(seed)
+        need = [-(-kv // page) for _, kv in lens]
+        self.P = sum(need) + spare
+        order = rng.permutation(self.P)
+        M = max(need + [1]) + extra_cols
+        table = np.full((len(lens), M), -7, np.int32)  # entries past a sequence's pages are never read
+        at = 0
+        for b, n in enumerate(need):
+            table[b, :n] = order[at:at + n]
+            at += n
+        self.table_host = table
+        self.free = order[at:]
+        self.table = torch.from_numpy(table).cuda()
+        self.cu_host = np.concatenate([[0], np.cumsum([n for n, _ in lens])]).astype(np.int32)
+        self.cu = torch.from_numpy(self.cu_host).cuda()
+        self.kv_len = torch.tensor([kv for _, kv in lens], dtype=torch.int32, device="cuda")
+        self.T = int(self.cu_host[-1])
+        shape = (self.P, self.hkv, page, self.D) if heads_first else (self.P, page, self.hkv, self.D)
+        self.k, self.v = (self.rand(shape) for _ in range(2))
+        if heads_first:
+            self.k, self.v = self.k.transpose(1, 2), self.v.transpose(1, 2)
+        self.q = self.rand((self.T, self.hq, self.D), 2.0)
+        self.max_q, self.max_kv = max([n for n, _ in lens] + [1]), max([kv for _, kv in lens] + [1])
+
+    def rand(self, shape, scale=1.0):
+        return (scale * torch.randn(shape, generator=self.gen, device="cuda")).to(self.dt)
+
+    def rows(self, b, positions):
+        """(page, row) of positions of sequence b"""
+        return self.table_host[b, positions // self.page], positions % self.page
+
+    def gathered(self, pages, b):
+        page, row = self.rows(b, np.arange(self.lens[b][1]))
+        return pages[torch.from_numpy(page.astype(np.int64)).cuda(), torch.from_numpy(row).cuda()].double()
+
+    def attend(self, G, **kw):
+        kw.setdefault("max_q", self.max_q)
+        kw.setdefault("max_kv", self.max_kv)
+        return G.attend(self.q, self.k, self.v, self.table, self.kv_len, self.cu, **kw)
+
+
+def reference(bt, window=0, scale=None):
+    """out, lse in 64 bits and the bounds of both"""
+    scale = bt.D ** -0.5 if scale is None else scale
+    group, u = bt.hq // bt.hkv, U[bt.dt]
+    out = torch.zeros((bt.T, bt.hq, bt.D), dtype=torch.float64, device="cuda")
+    lse = torch.full((bt.T, bt.hq), -math.inf, dtype=torch.float64, device="cuda")
+    out_tol, lse_tol = torch.zeros_like(out), torch.zeros_like(lse)
+    for b, (n, kv) in enumerate(bt.lens):
+        if n == 0:
+            continue
+        k, v = bt.gathered(bt.k, b), bt.gathered(bt.v, b)
+        at = int(bt.cu_host[b])
+        pos = torch.arange(kv - n, kv, device="cuda")[:, None]
+        key = torch.arange(kv, device="cuda")[None]
+        seen = (key <= pos) & ((key > pos - window) if window else (key >= 0))
+        for h in range(bt.hq):
+            g = h // group
+            q = bt.q[at:at + n, h].double()
+            kg = torch.nan_to_num(k[:, g], 0, 0, 0)
+            x = scale * (q @ kg.T.contiguous())
+            e = (bt.D + 8) * 2.0 ** -24 * abs(scale) * (q.abs() @ kg.abs().T.contiguous())
+            x = torch.where(seen, x, -math.inf)
+            e = torch.where(seen, e, 0.0).amax(-1)
+            l = torch.logsumexp(x, -1)
+            p = torch.exp(x - l[:, None])
+            vg = torch.nan_to_num(v[:, g], 0, 0, 0)
+            o, mass = p @ vg, p @ vg.abs()
+            out[at:at + n, h], lse[at:at + n, h] = o, l
+            out_tol[at:at + n, h] = (u + 2 * e[:, None] + 2.0 ** -18) * mass + u * o.abs() + \
+                (kv * 2.0 ** -25 * vg.abs().max() + 2.0 ** -25 if bt.dt == torch.float16 else 0.0)
+            lse_tol[at:at + n, h] = e + 2.0 ** -20 * (1 + l.abs())
+    return out, lse, out_tol, lse_tol
+
+
+def agree(got, bt, rows=None, **kw):
+    out, lse, out_tol, lse_tol = reference(bt, **kw)
+    sel = slice(None) if rows is None else rows
+    d = (got[0].double() - out)[sel].abs()
+    assert bool((d <= out_tol[sel]).all()), float((d / out_tol[sel].clamp_min(1e-300)).nan_to_num(math.inf).max())
+    d = (got[1].double() - lse)[sel].abs()
+    assert bool((d <= lse_tol[sel]).all()), float((d / lse_tol[sel].clamp_min(1e-300)).nan_to_num(math.inf).max())
+
+
+MIXED = [(1, 1), (1, 700), (0, 33), (5, 5), (5, 130), (0, 0), (1, 64), (9, 65), (33, 200), (2, 1025)]
+
+
+@pytest.mark.parametrize("heads", [(28, 4, 128), (4, 4, 64), (15, 5, 64), (8, 1, 256), (32, 8, 128), (6, 2, 256),
+                                   (40, 1, 128)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_mixed_lengths(G, heads, dtype):
+    bt = Batch(MIXED, heads, 16, dtype, seed=1)
+    agree(bt.attend(G), bt)
+
+
+@pytest.mark.parametrize("page", [1, 3, 16, 24, 64, 100, 256, 4096])
+@pytest.mark.parametrize("window", [0, 1, 37, 128, 5000])
+def test_pages_and_windows(G, page, window):
+    bt = Batch([(1, 777), (7, 300), (70, 333), (3, 3), (0, 9), (1, 129)], (14, 2, 128), page, "bf16", seed=page)
+    agree(bt.attend(G, window=window), bt, window=window)
+
+
+@pytest.mark.parametrize("kv", [1, 2, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 511, 513, 2047, 4097])
+def test_single_tokens(G, kv):
+    """decoding, one token a sequence, lengths around every tile and split"""
+    bt = Batch([(1, kv), (1, max(1, kv // 2))], (28, 4, 128), 16, "bf16", seed=kv)
+    agree(bt.attend(G), bt)
+
+
+@pytest.mark.parametrize("n", [1, 2, 7, 8, 16, 31, 32, 33, 64, 127, 129, 300, 513])
+@pytest.mark.parametrize("heads", [(8, 1, 128), (3, 3, 64), (10, 2, 256)])
+def test_chunk_lengths(G, n, heads):
+    bt = Batch([(n, n), (n, n + 95)], heads, 32, "bf16", seed=n)
+    agree(bt.attend(G), bt)
+
+
+@pytest.mark.parametrize("lens", [[(1, 40000)], [(4, 70001), (1, 17)], [(40, 33333)], [(300, 20000), (1, 30000)]])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_long_caches(G, lens, dtype):
+    bt = Batch(lens, (16, 2, 128), 64, dtype, seed=5)
+    agree(bt.attend(G), bt)
+    agree(bt.attend(G, window=9000), bt, window=9000)
+
+
+def test_many_sequences(G):
+    lens = [(i % 4, 3 + 7 * i % 400) for i in range(300)]
+    bt = Batch(lens, (8, 2, 64), 16, "bf16", seed=6)
+    agree(bt.attend(G), bt)
+
+
+def test_bounds_larger_than_the_batch(G):
+    bt = Batch(MIXED, (28, 4, 128), 16, "bf16", seed=7, extra_cols=200)
+    agree(bt.attend(G, max_q=4000, max_kv=100000), bt)
+
+
+def test_scales_and_sharp_scores(G):
+    """scores of hundreds: the running maximum moves often and far"""
+    bt = Batch([(5, 900), (64, 400)], (8, 2, 128), 16, "bf16", seed=8)
+    for scale in (3.0, -1.0, 0.0, 1e-3):
+        agree(bt.attend(G, scale=scale), bt, scale=scale)
+    # keys in the order of their scores, rising and falling
+    one = Batch([(1, 600)], (1, 1, 64), 16, "f16", seed=9)
+    page, row = one.rows(0, np.arange(600))
+    for sign in (1.0, -1.0):
+        ramp = sign * torch.linspace(-8, 8, 600, device="cuda")[:, None] * torch.ones(64, device="cuda")
+        one.k[torch.from_numpy(page.astype(np.int64)).cuda(), torch.from_numpy(row).cuda(), 0] = ramp.half()
+        one.q.fill_(1.0)
+        agree(one.attend(G), one)
+
+
+def test_layouts(G):
+    """pages with their heads before their rows; queries and outputs inside larger arrays"""
+    for dtype in DT:
+        bt = Batch(MIXED, (6, 3, 64), 16, dtype, seed=10, heads_first=True)
+        agree(bt.attend(G), bt)
+        wide = bt.rand((bt.T, 20, bt.D))
+        wide[:, 5:11] = bt.q
+        bt.q = wide[:, 5:11]
+        out = torch.zeros((bt.T, 9, bt.D), dtype=bt.dt, device="cuda")
+        lse = torch.zeros((bt.T, 6), device="cuda")
+        got = bt.attend(G, out=out[:, 2:8], lse=lse)
+        assert got[1] is lse and bool((out[:, :2] == 0).all()) and bool((out[:, 8:] == 0).all())
+        agree(got, bt)
+
+
+@pytest.mark.parametrize("poison", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("lens", [[(5, 130), (1, 31), (33, 90)], [(200, 300)], [(3, 3)]])
+def test_what_is_not_seen_has_no_part(G, poison, lens):
+    """infinities and NaN in free pages, after a sequence's end, before its window, and in the chunk's later tokens"""
+    window = 40
+    bt = Batch(lens, (8, 2, 128), 16, "bf16", seed=11, spare=3)
+    clean = bt.attend(G, window=window)
+    for pages in (bt.k, bt.v):
+        pages[torch.from_numpy(bt.free.astype(np.int64)).cuda()] = poison
+        for b, (n, kv) in enumerate(lens):
+            if kv % bt.page:
+                pages[int(bt.table_host[b, kv // bt.page]), kv % bt.page:] = poison
+            for s in range(0, max(0, kv - n - window)):
+                page, row = bt.rows(b, np.array([s]))
+                pages[int(page[0]), int(row[0])] = poison
+    got = bt.attend(G, window=window)
+    assert torch.equal(got[0], clean[0]) and torch.equal(got[1], clean[1])
+    # each sequence's last key: only its last token sees it
+    for pages in (bt.k, bt.v):
+        for b, (n, kv) in enumerate(lens):
+            page, row = bt.rows(b, np.array([kv - 1]))
+            pages[int(page[0]), int(row[0])] = poison
+    got = bt.attend(G, window=window)
+    last = torch.zeros(bt.T, dtype=torch.bool)
+    last[bt.cu_host[1:] - 1] = True
+    assert torch.equal(got[0][~last], clean[0][~last]) and torch.equal(got[1][~last], clean[1][~last])
+    assert not torch.isfinite(got[0][last].float()).all(-1).any()
+
+
+def test_a_seen_infinity_is_seen(G):
+    bt = Batch([(4, 50)], (2, 1, 64), 16, "bf16", seed=12)
+    page, row = bt.rows(0, np.array([48]))
+    bt.v[int(page[0]), int(row[0]), 0, 3] = math.inf
+    out, _ = bt.attend(G)
+    assert bool(torch.isposinf(out[2:, :, 3].float()).all()) and bool(torch.isfinite(out[:2].float()).all())
+
+
+def test_bad_sequences_are_nan(G):
+    lens = [(2, 90), (1, 40), (3, 64), (1, 100), (40, 200)]
+
+    def check(bt, bad, last=0, **kw):
+        """the rows of these sequences are NaN (of the last one at least that many)"""
+        got = bt.attend(G, **kw)
+        rows = torch.zeros(bt.T, dtype=torch.bool, device="cuda")
+        for b in bad:
+            rows[int(bt.cu_host[b]):int(bt.cu_host[b + 1])] = True
+        good = Batch(lens, (8, 2, 128), 16, "bf16", seed=13)
+        agree(got, good, rows=~rows)
+        if last:
+            rows[int(bt.cu_host[bad[-1]]):int(bt.cu_host[bad[-1] + 1]) - last] = False
+        assert bool(torch.isnan(got[0][rows].float()).all()) and bool(torch.isnan(got[1][rows]).all())
+
+    def fresh():
+        return Batch(lens, (8, 2, 128), 16, "bf16", seed=13)
+
+    bt = fresh()
+    bt.table[0, 1] = bt.P
+    bt.table[4, 12] = -1
+    check(bt, [0, 4], last=8)  # positions 192 .. 199 are on the missing page
+    bt = fresh()
+    bt.kv_len[1] = 1 << 30
+    check(bt, [1])
+    bt = fresh()
+    bt.kv_len[2] = 2
+    check(bt, [2])
+    check(fresh(), [3, 4], max_kv=99)
+    check(fresh(), [4], max_q=3)
+    bt = fresh()
+    bt.cu[5] = 10000  # the last chunk reaches past the packed rows
+    check(bt, [4])
+
+
+def test_rows_of_no_sequence_are_left(G):
+    bt = Batch([(3, 20), (2, 70)], (4, 2, 64), 16, "bf16", seed=14)
+    bt.q = bt.rand((bt.T + 6, bt.hq, bt.D))
+    out = torch.full_like(bt.q, 7.0)
+    lse = torch.full((bt.T + 6, bt.hq), 7.0, device="cuda")
+    bt.cu = bt.cu + 2
+    bt.attend(G, out=out, lse=lse)
+    assert bool((out[:2] == 7).all()) and bool((out[bt.T + 2:] == 7).all())
+    assert bool((lse[:2] == 7).all()) and bool((lse[bt.T + 2:] == 7).all())
+    bt.q = bt.q[2:bt.T + 2]
+    agree((out[2:bt.T + 2], lse[2:bt.T + 2]), bt)
+    empty = bt.q[:0]
+    got = G.attend(empty, bt.k, bt.v, bt.table, bt.kv_len, torch.zeros_like(bt.cu), 1, 100)
+    assert got[0].shape == (0, bt.hq, bt.D)
+
+
+def test_offsets_past_32_bits(G):
+    """a cache of more than 2^32 entries: the sequence's pages lie at its end"""
+    page, H, D = 64, 8, 128
+    P = (1 << 32) // (page * H * D) + 40
+    bt = Batch([(3, 1500)], (16, H, D), page, "bf16", seed=15)
+    k, v = bt.k, bt.v
+    n = k.shape[0]
+    big_k, big_v = (torch.empty((P, page, H, D), dtype=bt.dt, device="cuda") for _ in range(2))
+    big_k[-n:], big_v[-n:] = k, v
+    want = bt.attend(G)
+    got = G.attend(bt.q, big_k, big_v, bt.table + (P - n), bt.kv_len, bt.cu, bt.max_q, bt.max_kv)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    new_k, new_v = bt.rand((3, H, D)), bt.rand((3, H, D))
+    G.kv_append(new_k, new_v, big_k, big_v, bt.table + (P - n), bt.kv_len, bt.cu)
+    G.kv_append(new_k, new_v, bt.k, bt.v, bt.table, bt.kv_len, bt.cu)
+    assert torch.equal(big_k[-n:], bt.k) and torch.equal(big_v[-n:], bt.v)
+
+
+def test_same_bits_every_time(G):
+    bt = Batch([(1, 9000), (5, 3000), (1, 1)], (28, 4, 128), 16, "bf16", seed=16)
+    first = bt.attend(G)
+    for _ in range(5):
+        again = bt.attend(G)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_other_stream_and_graph(G):
+    bt = Batch([(2, 5000), (1, 300), (6, 900)], (28, 4, 128), 16, "bf16", seed=17)
+    want = bt.attend(G)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = bt.attend(G, stream=side)
+    side.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    k, v = bt.rand((bt.T, bt.hkv, bt.D)), bt.rand((bt.T, bt.hkv, bt.D))
+    out, lse = torch.empty_like(want[0]), torch.empty_like(want[1])
+    workspace = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        G.kv_append(k, v, bt.k, bt.v, bt.table, bt.kv_len, bt.cu, q=bt.q, q_out=bt.q)
+        bt.attend(G, out=out, lse=lse, workspace=workspace)
+    for i in range(4):
+        k.copy_(bt.rand(k.shape))
+        v.copy_(bt.rand(v.shape))
+        bt.q.copy_(bt.rand(bt.q.shape))
+        workspace.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        agree((out, lse), bt)
+
+
+# ------------------------------------------------------------------------------------------------------------ append
+def tables(n, rot, gen=None):
+    angle = torch.arange(n, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(rot // 2, dtype=torch.float64) * 2 / rot)
+    return angle.cos().float().cuda(), angle.sin().float().cuda()
+
+
+def turned(x, pos, weight, eps, cos, sin, interleaved):
+    """x [T, H, D] in 64 bits after norm and rotation, and the size of what was added up"""
+    x = x.double()
+    if weight is not None:
+        x = x / torch.sqrt((x * x).mean(-1, keepdim=True) + eps) * weight.double()
+    size = x.abs()
+    if cos is not None:
+        half = cos.shape[1]
+        a, c = (slice(0, 2 * half, 2), slice(1, 2 * half, 2)) if interleaved else (slice(0, half), slice(half, 2 * half))
+        cs, sn = cos.double()[pos][:, None], sin.double()[pos][:, None]
+        y = x.clone()
+        y[..., a], y[..., c] = x[..., a] * cs - x[..., c] * sn, x[..., c] * cs + x[..., a] * sn
+        s = x[..., a].abs() + x[..., c].abs()
+        size[..., a], size[..., c] = s, s
+        x = y
+    return x, size
+
+
+def rounded_once(got, want, size):
+    u = U[got.dtype]
+    assert bool(((got.double() - want).abs() <= u * want.abs() + 2.0 ** -20 * size + 2.0 ** -25).all())
+
+
+@pytest.mark.parametrize("heads", [(28, 4, 128), (4, 4, 64), (15, 5, 64), (8, 1, 256), (6, 2, 80), (3, 1, 8), (5, 5, 192)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("style", ["none", "half", "pairs"])
+def test_append(G, heads, dtype, norm, style):
+    D = heads[2]
+    lens = [(1, 1), (5, 100), (0, 40), (1, 77), (0, 0), (37, 60), (2, 2)]
+    bt = Batch(lens, heads, 24, dtype, seed=D)
+    k, v = bt.rand((bt.T, bt.hkv, D), 3.0), bt.rand((bt.T, bt.hkv, D))
+    weights = [1 + torch.randn(D, device="cuda") for _ in range(2)] if norm else [None, None]
+    pos = torch.cat([torch.arange(kv - n, kv) for n, kv in lens]).cuda()
+    page = np.concatenate([bt.rows(b, np.arange(kv - n, kv))[0] for b, (n, kv) in enumerate(lens)])
+    row = np.concatenate([bt.rows(b, np.arange(kv - n, kv))[1] for b, (n, kv) in enumerate(lens)])
+    page, row = torch.from_numpy(page.astype(np.int64)).cuda(), torch.from_numpy(row.astype(np.int64)).cuda()
+    for rot in sorted({0} if style == "none" else {16 if style == "half" and D >= 16 else 8, D // 16 * 16 if D >= 16 else 8}):
+        if style == "half" and rot % 16:
+            continue
+        cos, sin = tables(101, rot) if rot else (None, None)
+        old_k, old_v = bt.k.clone(), bt.v.clone()
+        status = torch.full((len(lens),), -1, dtype=torch.int32, device="cuda")
+        q_out, _ = G.kv_append(k, v, bt.k, bt.v, bt.table, bt.kv_len, bt.cu, q=bt.q, cos=cos, sin=sin,
+                               interleaved=style == "pairs", q_norm=weights[0], k_norm=weights[1], eps=1e-5, status=status)
+        assert bool((status == 0).all())
+        want, size = turned(k, pos, weights[1], 1e-5, cos, sin, style == "pairs")
+        rounded_once(bt.k[page, row], want, size)
+        want, size = turned(bt.q, pos, weights[0], 1e-5, cos, sin, style == "pairs")
+        rounded_once(q_out, want, size)
+        assert torch.equal(bt.v[page, row], v)
+        if not norm and not rot:
+            assert torch.equal(bt.k[page, row], k) and torch.equal(q_out, bt.q)
+        # nothing else was written
+        old_k[page, row], old_v[page, row] = bt.k[page, row], bt.v[page, row]
+        assert torch.equal(bt.k, old_k) and torch.equal(bt.v, old_v)
+
+
+def test_append_in_place_strided_and_alone(G):
+    """keys, values and queries as slices of one projection; queries turned in place; and no queries at all"""
+    bt = Batch([(3, 30), (1, 9), (64, 64)], (6, 2, 128), 16, "bf16", seed=20, heads_first=True)
+    qkv = bt.rand((bt.T, 10, 128))
+    cos, sin = tables(64, 128)
+    pos = torch.cat([torch.arange(kv - n, kv) for n, kv in bt.lens]).cuda()
+    before = qkv.clone()
+    G.kv_append(qkv[:, 6:8], qkv[:, 8:], bt.k, bt.v, bt.table, bt.kv_len, bt.cu, q=qkv[:, :6], q_out=qkv[:, :6],
+                cos=cos, sin=sin)
+    assert torch.equal(qkv[:, 6:], before[:, 6:])
+    want, size = turned(before[:, :6], pos, None, 0, cos, sin, False)
+    rounded_once(qkv[:, :6], want, size)
+    page = np.concatenate([bt.rows(b, np.arange(kv - n, kv))[0] for b, (n, kv) in enumerate(bt.lens)])
+    row = np.concatenate([bt.rows(b, np.arange(kv - n, kv))[1] for b, (n, kv) in enumerate(bt.lens)])
+    page, row = torch.from_numpy(page.astype(np.int64)).cuda(), torch.from_numpy(row.astype(np.int64)).cuda()
+    with_q = bt.k[page, row].clone()
+    bt.k.zero_()
+    assert G.kv_append(qkv[:, 6:8], qkv[:, 8:], bt.k, bt.v, bt.table, bt.kv_len, bt.cu, cos=cos, sin=sin)[0] is None
+    assert torch.equal(bt.k[page, row], with_q) and torch.equal(bt.v[page, row], qkv[:, 8:])
+
+
+def test_append_leaves_out_what_has_no_place(G):
+    lens = [(2, 40), (3, 33), (4, 50), (1, 10), (2, 64)]
+    bt = Batch(lens, (2, 1, 64), 16, "bf16", seed=21)
+    k, v = bt.rand((bt.T + 5, 1, 64)), bt.rand((bt.T + 5, 1, 64))  # five rows of no sequence
+    cos, sin = tables(48, 64)
+    bt.table[1, 2] = bt.P          # position 32: the last of its chunk
+    bt.kv_len[3] = 1 << 20         # beyond the table
+    old_k, old_v = bt.k.clone(), bt.v.clone()
+    status = torch.full((5,), -1, dtype=torch.int32, device="cuda")
+    G.kv_append(k, v, bt.k, bt.v, bt.table, bt.kv_len, bt.cu, cos=cos, sin=sin, status=status)
+    assert status.tolist() == [0, 2, 2, 2, 2]
+    pos = {0: [38, 39], 1: [30, 31], 2: [46, 47]}  # 2: positions 48, 49 have no rotation; 4: neither has
+    for b, places in pos.items():
+        page, row = bt.rows(b, np.array(places))
+        at = int(bt.cu_host[b])
+        want, size = turned(k[at:at + 2], torch.tensor(places).cuda(), None, 0, cos, sin, False)
+        p, r = torch.from_numpy(page.astype(np.int64)).cuda(), torch.from_numpy(row).cuda()
+        rounded_once(bt.k[p, r], want, size)
+        assert torch.equal(bt.v[p, r], v[at:at + 2])
+        old_k[p, r], old_v[p, r] = bt.k[p, r], bt.v[p, r]
+    assert torch.equal(bt.k, old_k) and torch.equal(bt.v, old_v)
