@@ -569,8 +569,9 @@ int grid_apply(const uint32_t* mask_dev, void* logits_dev, int32_t dtype, int32_
 /* A cache in caller-owned device memory: entry (page, row, head, i) of the
  * keys is k_pages[page * k_stride[0] + row * k_stride[1] + head * k_stride[2]
  * + i], of the values likewise with v_stride (strides in elements, multiples
- * of 8, not negative; pages 16-byte aligned).  So a page may hold its rows
- * before its heads or its heads before its rows. */
+ * of 8, not negative, of pages below 2^31, of rows and heads below 2^27; pages
+ * 16-byte aligned).  So a page may hold its rows before its heads or its heads
+ * before its rows. */
 typedef struct {
   void* k_pages;        /* device, dtype */
   void* v_pages;        /* device, dtype */

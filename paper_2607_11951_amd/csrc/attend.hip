@@ -68,12 +68,17 @@ __device__ inline float other_half(float x) {  // the value of lane ^ 32
   return (threadIdx.x & 32) ? __uint_as_float(r[0]) : __uint_as_float(r[1]);
 }
 
-// 16 bytes a lane from global memory to LDS at `to` + 16 * lane (to: uniform, bytes from the start of LDS).  Written
-// as assembly because the compiler waits for all such loads before any LDS read; they are counted by vmcnt.
+// 16 bytes a lane from global memory (uniform base + the lane's offset in bytes) to LDS at `to` + 16 * lane (to:
+// uniform, bytes from the start of LDS).  Written as assembly because the compiler waits for all such loads before any
+// LDS read; they are counted by vmcnt.  LDS reads issued before are waited for first: they may be of what is overwritten.
+__device__ inline void to_lds(const void* base, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to) : "memory");
+}
 __device__ inline void to_lds(const void* from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
 }
-__device__ inline void wait_lds() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ inline void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 #define GRID_LDS __attribute__((address_space(3)))
 
@@ -84,17 +89,23 @@ __device__ constexpr int swz(int row) {
   return D == 64 ? ((row >> 1 & 1) << 2 | (row >> 2 & 3)) : ((row & 3) << 2 | (row >> 2 & 3));
 }
 
-// RW x KW waves: RW * 32 rows, stages of KW * KT keys of which a wave takes KT.
-template <typename T, int D, int RW, int KW, int KT>
-__global__ __launch_bounds__(64 * RW * KW) void tile_kernel(Paged P, AttendArgs a) {
+// RW x KW waves: RW * 32 rows, stages of KW * KT keys of which a wave takes KT.  With one wave of rows a wave loads its
+// own keys and waits for nobody; otherwise the stage is shared.  DEPTH stages are held.  UNI: the rows that one load
+// instruction brings (64 / PR) lie in one page, so their address is a scalar and an offset that does not change.
+template <typename T, int D, int RW, int KW, int KT, int DEPTH, int WGS, bool UNI>
+__global__ __launch_bounds__(64 * RW * KW, RW * KW * WGS / 4) void tile_kernel(Paged P, AttendArgs a) {
   typedef typename Vec<T>::eight Eight;
   constexpr int W = RW * KW, NT = 64 * W, TM = 32 * RW, SK = KW * KT;
   constexpr int PR = D / 8;               // 16-byte pieces of a row
+  constexpr int RPI = 64 / PR;            // rows that one load instruction brings
   constexpr int LOADS = SK * PR / NT;     // of the keys, as many of the values, a thread
   constexpr int KB = KT / 32, DB = D / 32, QS = D / 16;
+  constexpr bool PRIV = RW == 1;
   constexpr uint32_t kHalf = SK * D * 2;  // bytes of a stage's keys
-  static_assert(SK * PR % NT == 0 && 128 % SK == 0, "");
-  __shared__ __attribute__((aligned(16))) uint8_t lds[4 * kHalf];
+  constexpr uint32_t kMerge = KW == 1 ? 0 : KW * TM * (2 + D / 2 + 4) * 4;  // what waves of other keys meet in
+  constexpr uint32_t kLds = DEPTH * 2 * kHalf > kMerge ? DEPTH * 2 * kHalf : kMerge;
+  static_assert(SK * PR % NT == 0 && 128 % SK == 0 && KT % RPI == 0, "");
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kLds];
 
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % RW, kw = wave / RW, half = lane >> 5, col = lane & 31;
@@ -151,29 +162,51 @@ __global__ __launch_bounds__(64 * RW * KW) void tile_kernel(Paged P, AttendArgs 
     }
   }
 
-  // stage addresses: thread's piece i is piece (i * NT + tid) of the stage
+  // Stage rows: load i of a wave brings RPI rows from row_of(i) on, a lane piece `lane % PR` of row `lane / PR`.
+  const auto row_of = [&](int i) { return PRIV ? kw * KT + i * RPI : (i * W + wave) * RPI; };
+  const uint32_t base = (uint32_t)(uintptr_t)(GRID_LDS uint8_t*)lds;
+  const int lrow = lane / PR;
   int32_t page[LOADS];
   uint32_t row[LOADS];
   bool missing = false;
-  auto find = [&](int s0) {
+  const auto find = [&](int s0) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int s = min(s0 + (i * NT + tid) / PR, s_hi - 1);
-      page[i] = P.page_of(b, (uint32_t)s, row[i]);
+      if constexpr (UNI) {
+        const uint32_t s = (uint32_t)min(s0 + row_of(i), (s_hi - 1) / RPI * RPI);
+        const uint32_t c = P.page.quot(s);
+        row[i] = s - c * P.page.d;
+        page[i] = ((const __attribute__((address_space(4))) int32_t*)(P.table + (int64_t)b * P.table_stride))[c];
+      } else {
+        page[i] = P.page_of(b, (uint32_t)min(s0 + row_of(i) + lrow, s_hi - 1), row[i]);
+      }
     }
   };
-  const uint32_t base = (uint32_t)(uintptr_t)(GRID_LDS uint8_t*)lds;
-  auto fetch = [&](int buf) {
+  const auto fetch = [&](int s0, int buf) {
+    if constexpr (PRIV) wait_reads();
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const int at = i * NT + tid, rr = at / PR, piece = at % PR ^ swz<D>(rr);
+      const int rr = row_of(i) + lrow, piece = lane % PR ^ swz<D>(rr);
       const bool in = P.in_cache(page[i]);
       missing |= !in;
-      const int64_t pg = in ? page[i] : 0;
-      const uint32_t to = base + (uint32_t)buf * 2 * kHalf + (uint32_t)(i * NT + wave * 64) * 16;
-      to_lds(P.k + pg * P.ks[0] + row[i] * P.ks[1] + g * P.ks[2] + piece * 8, __builtin_amdgcn_readfirstlane(to));
-      to_lds(P.v + pg * P.vs[0] + row[i] * P.vs[1] + g * P.vs[2] + piece * 8, __builtin_amdgcn_readfirstlane(to + kHalf));
+      const uint32_t pg = in ? (uint32_t)page[i] : 0u;
+      const uint32_t to = base + (uint32_t)buf * 2 * kHalf + (uint32_t)row_of(i) * D * 2;
+      const uint16_t* k = P.k + (uint64_t)pg * (uint32_t)P.ks[0] + (uint64_t)row[i] * (uint32_t)P.ks[1] + g * P.ks[2];
+      const uint16_t* v = P.v + (uint64_t)pg * (uint32_t)P.vs[0] + (uint64_t)row[i] * (uint32_t)P.vs[1] + g * P.vs[2];
+      if constexpr (UNI) {
+        // rows at and after s_hi: the last row again
+        const uint32_t r = (uint32_t)min(lrow, s_hi - 1 - min(s0 + row_of(i), (s_hi - 1) / RPI * RPI));
+        to_lds(k, (r * (uint32_t)P.ks[1] + piece * 8) * 2, to);
+        to_lds(v, (r * (uint32_t)P.vs[1] + piece * 8) * 2, to + kHalf);
+      } else {
+        to_lds(k + piece * 8, to);
+        to_lds(v + piece * 8, to + kHalf);
+      }
     }
+  };
+  const auto arrived = [&] {
+    wait_loads();
+    if constexpr (!PRIV) __syncthreads();
   };
 
   float16_v o[DB];
@@ -184,15 +217,22 @@ __global__ __launch_bounds__(64 * RW * KW) void tile_kernel(Paged P, AttendArgs 
   float m = -INFINITY, l = 0.f;
 
   find(s_lo);
-  fetch(0);
-  if (s_lo + SK < s_hi) find(s_lo + SK);
-  wait_lds();
-  __syncthreads();
+  if constexpr (DEPTH > 1) {
+    fetch(s_lo, 0);
+    if (s_lo + SK < s_hi) find(s_lo + SK);
+    arrived();
+  }
   int buf = 0;
-  for (int s0 = s_lo; s0 < s_hi; s0 += SK, buf ^= 1) {
-    if (s0 + SK < s_hi) {
-      fetch(buf ^ 1);
-      if (s0 + 2 * SK < s_hi) find(s0 + 2 * SK);
+  for (int s0 = s_lo; s0 < s_hi; s0 += SK, buf ^= DEPTH - 1) {
+    if constexpr (DEPTH > 1) {
+      if (s0 + SK < s_hi) {
+        fetch(s0 + SK, buf ^ 1);
+        if (s0 + 2 * SK < s_hi) find(s0 + 2 * SK);
+      }
+    } else {
+      fetch(s0, 0);
+      if (s0 + SK < s_hi) find(s0 + SK);
+      arrived();
     }
     const int k0 = s0 + kw * KT;  // this wave's keys
     const bool work = alive && k0 <= pos_max && k0 < s_hi && (!a.window || k0 + KT > pos_min - a.window + 1);
@@ -313,8 +353,10 @@ __global__ __launch_bounds__(64 * RW * KW) void tile_kernel(Paged P, AttendArgs 
         }
       }
     }
-    wait_lds();
-    __syncthreads();
+    if constexpr (DEPTH > 1)
+      arrived();
+    else if constexpr (!PRIV)
+      __syncthreads();
   }
   l += other_half(l);
   missing = __syncthreads_or(missing);
@@ -323,9 +365,9 @@ __global__ __launch_bounds__(64 * RW * KW) void tile_kernel(Paged P, AttendArgs 
 
   // waves that took other keys of the same rows: their sums meet in LDS
   if constexpr (KW > 1) {
-    float* ml = (float*)lds;                    // [KW][2][TM]
-    float* os = (float*)(lds + KW * 2 * TM * 4);  // [KW][TM][D + 4]
-    static_assert(KW * 2 * TM * 4 + KW * TM * (D + 4) * 4 <= 4 * kHalf, "");
+    constexpr int DH = D / 2;                     // in two halves of the entries, for room
+    float* ml = (float*)lds;                      // [KW][2][TM]
+    float* os = (float*)(lds + KW * 2 * TM * 4);  // [KW][TM][DH + 4]
     if (half == 0) {
       ml[(kw * 2 + 0) * TM + rw * 32 + col] = mc;
       ml[(kw * 2 + 1) * TM + rw * 32 + col] = l;
@@ -339,45 +381,51 @@ __global__ __launch_bounds__(64 * RW * KW) void tile_kernel(Paged P, AttendArgs 
     for (int w = 0; w < KW; ++w)
       sum += ml[(w * 2 + 1) * TM + rw * 32 + col] * __builtin_amdgcn_exp2f(ml[w * 2 * TM + rw * 32 + col] - ref);
     const float keep = __builtin_amdgcn_exp2f(mc - ref);
-    float* mine = os + (kw * TM + rw * 32 + col) * (D + 4);
-#pragma unroll
-    for (int d = 0; d < DB; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *(float4*)(mine + d * 32 + 2 * i + 4 * half) =
-            make_float4(o[d][i] * keep, o[d][i + 1] * keep, o[d][i + 2] * keep, o[d][i + 3] * keep);
     mc = top;
     l = sum;
     __syncthreads();
-    // a wave adds up a part of its rows' entries
-    constexpr int PART = 32 * D / 4 / 64 / KW;  // float4s a lane
     if (kw == 0 && half == 0) {
       ml[rw * 32 + col] = mc;
       ml[TM + rw * 32 + col] = l;
     }
-    __syncthreads();
+    float* mine = os + (kw * TM + rw * 32 + col) * (DH + 4);
+    constexpr int PART = 32 * DH / 4 / 64 / KW;  // float4s a lane
 #pragma unroll
-    for (int j = 0; j < PART; ++j) {
-      const int at = (j * KW + kw) * 64 + lane, rr = rw * 32 + at / (D / 4), e = at % (D / 4) * 4;
-      if (tile * TM + rr >= rows) continue;
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int hd = 0; hd < 2; ++hd) {
 #pragma unroll
-      for (int w = 0; w < KW; ++w) {
-        const float4 y = *(const float4*)(os + (w * TM + rr) * (D + 4) + e);
-        x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
+      for (int d = 0; d < DB / 2; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const float16_v& x = o[hd * (DB / 2) + d];
+          *(float4*)(mine + d * 32 + 2 * i + 4 * half) =
+              make_float4(x[i] * keep, x[i + 1] * keep, x[i + 2] * keep, x[i + 3] * keep);
+        }
+      __syncthreads();
+      // a wave adds up a part of its rows' entries
+#pragma unroll
+      for (int j = 0; j < PART; ++j) {
+        const int at = (j * KW + kw) * 64 + lane, rr = rw * 32 + at / (DH / 4), e = at % (DH / 4) * 4;
+        if (tile * TM + rr >= rows) continue;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < KW; ++w) {
+          const float4 y = *(const float4*)(os + (w * TM + rr) * (DH + 4) + e);
+          x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
+        }
+        const int i = (int)a.group.quot((uint32_t)(tile * TM + rr)), h = g * G + tile * TM + rr - i * G, t = ch.first + i;
+        const float rm = ml[rr], rl = ml[TM + rr];
+        if (whole) {
+          const float over = rl == 0.f ? 0.f : 1.f / rl;
+          T y[4] = {(T)(x.x * over), (T)(x.y * over), (T)(x.z * over), (T)(x.w * over)};
+          *(uint2*)(a.out + t * a.os[0] + h * a.os[1] + hd * DH + e) = *(uint2*)y;
+          if (a.lse && e == 0 && hd == 0) a.lse[(int64_t)t * a.hq + h] = (rm + __builtin_amdgcn_logf(rl)) * kLn2;
+        } else {
+          const int64_t slot = ((int64_t)split * P.T + t) * a.hq + h;
+          *(float4*)(a.part_o + slot * D + hd * DH + e) = x;
+          if (e == 0 && hd == 0) a.part_ml[slot] = make_float2(rm, rl);
+        }
       }
-      const int i = (int)a.group.quot((uint32_t)(tile * TM + rr)), h = g * G + tile * TM + rr - i * G, t = ch.first + i;
-      const float rm = ml[rr], rl = ml[TM + rr];
-      if (whole) {
-        const float over = rl == 0.f ? 0.f : 1.f / rl;
-        T y[4] = {(T)(x.x * over), (T)(x.y * over), (T)(x.z * over), (T)(x.w * over)};
-        *(uint2*)(a.out + t * a.os[0] + h * a.os[1] + e) = *(uint2*)y;
-        if (a.lse && e == 0) a.lse[(int64_t)t * a.hq + h] = (rm + __builtin_amdgcn_logf(rl)) * kLn2;
-      } else {
-        const int64_t slot = ((int64_t)split * P.T + t) * a.hq + h;
-        *(float4*)(a.part_o + slot * D + e) = x;
-        if (e == 0) a.part_ml[slot] = make_float2(rm, rl);
-      }
+      if (hd == 0) __syncthreads();
     }
   } else {
     if (r0 + col >= rows) return;
@@ -405,13 +453,12 @@ __global__ __launch_bounds__(64 * RW * KW) void tile_kernel(Paged P, AttendArgs 
   }
 }
 
-// The splits of a row joined: a wave a token and head.
+// The splits of a row joined: a workgroup a token and head, D / 4 lanes a split, several splits side by side.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void join_kernel(Paged P, AttendArgs a) {
-  const int lane = (int)threadIdx.x & 63;
-  const int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int t = (int)(u / a.hq), h = (int)(u % a.hq);
-  if (t >= P.T) return;
+  constexpr int L = D / 4, N = 256 / L;
+  const int tid = (int)threadIdx.x, lane = tid & 63, e = tid % L * 4, side = tid / L;
+  const int t = (int)(blockIdx.x / (uint32_t)a.hq), h = (int)(blockIdx.x % (uint32_t)a.hq);
   int b = 0;
   for (int s = 0; s < P.B; s += 64) b += __popcll(__ballot(s + lane < P.B && P.cu_q[s + lane + 1] <= t));
   if (b >= P.B) return;
@@ -421,24 +468,34 @@ __global__ __launch_bounds__(256) void join_kernel(Paged P, AttendArgs a) {
   if (ch.kv - start <= a.len) return;
   const int pos = ch.kv - ch.n + t - ch.first;
   const int from = (max(a.window ? pos - a.window + 1 : 0, start) - start) / a.len, to = (pos - start) / a.len;
-  constexpr int E = D / 64;
-  float m = -INFINITY, l = 0.f, o[E] = {};
-  for (int s = from; s <= to; ++s) {
+  float m = -INFINITY, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  const auto take = [&](float om, float ol, float4 x) {
+    const float now = fmaxf(m, om), ref = now == -INFINITY ? 0.f : now;
+    const float keep = __builtin_amdgcn_exp2f(m - ref), add = __builtin_amdgcn_exp2f(om - ref);
+    l = l * keep + ol * add;
+    o.x = o.x * keep + x.x * add, o.y = o.y * keep + x.y * add;
+    o.z = o.z * keep + x.z * add, o.w = o.w * keep + x.w * add;
+    m = now;
+  };
+#pragma unroll 4
+  for (int s = from + side; s <= to; s += N) {
     const int64_t slot = ((int64_t)s * P.T + t) * a.hq + h;
     const float2 p = a.part_ml[slot];
-    const float now = fmaxf(m, p.x), ref = now == -INFINITY ? 0.f : now;
-    const float keep = __builtin_amdgcn_exp2f(m - ref), add = __builtin_amdgcn_exp2f(p.x - ref);
-    l = l * keep + p.y * add;
-#pragma unroll
-    for (int i = 0; i < E; ++i) o[i] = o[i] * keep + a.part_o[slot * D + lane * E + i] * add;
-    m = now;
+    take(p.x, p.y, *(const float4*)(a.part_o + slot * D + e));
   }
-  const float over = l == 0.f ? 0.f : 1.f / l;
-  T y[E];
+  __shared__ float2 ml[N];
+  __shared__ float4 os[N][L];
+  if (e == 0) ml[side] = make_float2(m, l);
+  os[side][tid % L] = o;
+  __syncthreads();
+  if (side > 0) return;
 #pragma unroll
-  for (int i = 0; i < E; ++i) y[i] = (T)(o[i] * over);
-  __builtin_memcpy(a.out + t * a.os[0] + h * a.os[1] + lane * E, y, sizeof(y));
-  if (a.lse && lane == 0) a.lse[(int64_t)t * a.hq + h] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+  for (int n = 1; n < N; ++n) take(ml[n].x, ml[n].y, os[n][tid]);
+  const float over = l == 0.f ? 0.f : 1.f / l;
+  T y[4] = {(T)(o.x * over), (T)(o.y * over), (T)(o.z * over), (T)(o.w * over)};
+  *(uint2*)(a.out + t * a.os[0] + h * a.os[1] + e) = *(uint2*)y;
+  if (a.lse && tid == 0) a.lse[(int64_t)t * a.hq + h] = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 int check(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_attend_args* g, bool pointers) {
@@ -460,8 +517,8 @@ int check(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_a
 }
 
 
-// Rows of a tile, and the ranges of keys: with few tiles the keys are split until there are about four workgroups a
-// compute unit, none with fewer keys than two stages.
+// Rows of a tile, and the ranges of keys: with few tiles the keys are split until there are about 4096 workgroups,
+// none with fewer than 256 keys.
 struct Shape {
   int tm, splits, len;
   int64_t tiles, blocks;
@@ -470,13 +527,12 @@ Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_atten
   Shape s;
   const int group = g->n_heads / c->n_kv_heads;
   const int64_t rows = (int64_t)std::min(g->max_q, std::max(1, x->n_tokens)) * group;
-  s.tm = rows <= 32 ? 32 : 128;
+  s.tm = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   s.tiles = (rows + s.tm - 1) / s.tm;
   const int64_t units = s.tiles * c->n_kv_heads * x->n_seqs;
   int64_t span = std::min<int64_t>(g->max_kv, (int64_t)x->table_cols * c->page_size);
   if (g->window) span = std::min<int64_t>(span, (int64_t)g->window + g->max_q + 127);
-  const int64_t want = std::max<int64_t>(1, 1024 / units);
-  s.len = (int)std::max<int64_t>(256, ((span + want - 1) / want + 127) / 128 * 128);
+  s.len = (int)std::min<int64_t>(std::max<int64_t>(256, (span * units / 1024 + 127) / 128 * 128), 32 * s.tm);
   s.splits = (int)((span + s.len - 1) / s.len);
   s.blocks = units * s.splits;
   return s;
@@ -487,23 +543,33 @@ size_t workspace_of(const grid_paged_cache* c, const grid_chunks* x, const grid_
   return (size_t)s.splits * (size_t)x->n_tokens * (size_t)g->n_heads * (size_t)(c->head_dim + 2) * 4;
 }
 
-template <typename T, int D, int RW, int KW, int KT>
+template <typename T, int D, int RW, int KW, int KT, int DEPTH, int WGS>
 void launch(const Paged& P, const AttendArgs& a, const Shape& s, hipStream_t stream) {
-  hipLaunchKernelGGL((tile_kernel<T, D, RW, KW, KT>), dim3((unsigned)s.blocks), dim3(64 * RW * KW), 0, stream, P, a);
+  const dim3 blocks((unsigned)s.blocks), threads(64 * RW * KW);
+  if (P.page.d % (512 / D) == 0)
+    hipLaunchKernelGGL((tile_kernel<T, D, RW, KW, KT, DEPTH, WGS, true>), blocks, threads, 0, stream, P, a);
+  else
+    hipLaunchKernelGGL((tile_kernel<T, D, RW, KW, KT, DEPTH, WGS, false>), blocks, threads, 0, stream, P, a);
   if (s.splits > 1) {
-    const int64_t waves = (int64_t)P.T * a.hq;
-    hipLaunchKernelGGL((join_kernel<T, D>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, P, a);
+    const dim3 rows((unsigned)P.T * (unsigned)a.hq);
+    hipLaunchKernelGGL((join_kernel<T, D>), rows, dim3(256), 0, stream, P, a);
   }
 }
 
 template <typename T>
 void choose(const Paged& P, const AttendArgs& a, const Shape& s, hipStream_t stream) {
   if (P.D == 64)
-    s.tm == 32 ? launch<T, 64, 1, 4, 32>(P, a, s, stream) : launch<T, 64, 4, 1, 64>(P, a, s, stream);
+    s.tm == 32   ? launch<T, 64, 1, 4, 32, 1, 2>(P, a, s, stream)
+    : s.tm == 64 ? launch<T, 64, 2, 2, 32, 1, 2>(P, a, s, stream)
+                 : launch<T, 64, 4, 1, 64, 2, 2>(P, a, s, stream);
   else if (P.D == 128)
-    s.tm == 32 ? launch<T, 128, 1, 4, 32>(P, a, s, stream) : launch<T, 128, 4, 1, 64>(P, a, s, stream);
+    s.tm == 32   ? launch<T, 128, 1, 4, 32, 1, 2>(P, a, s, stream)
+    : s.tm == 64 ? launch<T, 128, 2, 2, 32, 1, 2>(P, a, s, stream)
+                 : launch<T, 128, 4, 1, 64, 2, 2>(P, a, s, stream);
   else
-    s.tm == 32 ? launch<T, 256, 1, 2, 32>(P, a, s, stream) : launch<T, 256, 4, 1, 32>(P, a, s, stream);
+    s.tm == 32   ? launch<T, 256, 1, 4, 32, 1, 1>(P, a, s, stream)
+    : s.tm == 64 ? launch<T, 256, 2, 2, 32, 1, 1>(P, a, s, stream)
+                 : launch<T, 256, 4, 1, 32, 2, 1>(P, a, s, stream);
 }
 
 }  // namespace

@@ -25,6 +25,8 @@ int check_paged(const char* call, const grid_paged_cache* c, const grid_chunks* 
   if (!c->k_pages || !c->v_pages || !x->block_table || !x->kv_len || !x->cu_q) return bad("null pointer");
   if (!rows_fit(c->k_pages, c->k_stride, 3) || !rows_fit(c->v_pages, c->v_stride, 3))
     return bad("pages are 16-byte aligned, their strides multiples of 8");
+  for (const int64_t* s : {c->k_stride, c->v_stride})
+    if (s[0] >= (int64_t)1 << 31 || s[1] >= 1 << 27 || s[2] >= 1 << 27) return bad("strides");
   return GRID_OK;
 }
 
