@@ -48,20 +48,24 @@ struct AttendArgs {
   uint16_t* out;
   int64_t qs[2], os[2];
   float* lse;
-  float2* part_ml;  // [splits][tokens][heads]: maximum (in base 2 units of the scaled score), sum
-  float* part_o;    // [splits][tokens][heads][D], not divided by the sum
+  float2* part_ml;  // [slots][rows of a tile]: maximum (in base 2 units of the scaled score), sum
+  float* part_o;    // [slots][rows of a tile][D], not divided by the sum
+  int2* runs;       // [sequences][key heads]: first and last workgroup of the unit (few rows)
   Divisor group;
-  int32_t hq, max_q, max_kv, window, tiles, splits, len;  // len: keys of a split, a multiple of the stage
-  float c;          // |scale| * log2 e, above 0
-  bool negate;      // scale < 0: the queries are negated
+  int32_t hq, max_q, max_kv, window;
+  int32_t tiles, splits, len;  // many rows: tiles a sequence, ranges of len keys (a multiple of the stage)
+  float c;                     // |scale| * log2 e, above 0
+  bool negate;                 // scale < 0: the queries are negated
 };
 
 constexpr float kLn2 = 0.693147180559945309417f, kLog2e = 1.44269504088896340736f;
 
-// First key of the splits of a sequence: the window of its first new token, down to a whole stage of 128.
-__device__ inline int split_start(const AttendArgs& a, const Chunk& c) {
+// First key that a sequence's rows are given: the window of its first new token, down to a whole stage of 128.
+__device__ inline int first_key(const AttendArgs& a, const Chunk& c) {
   return a.window ? max(0, c.kv - c.n - a.window + 1) & ~127 : 0;
 }
+
+__device__ inline bool is_bad(const AttendArgs& a, const Chunk& c) { return !c.ok || c.n > a.max_q || c.kv > a.max_kv; }
 
 __device__ inline float other_half(float x) {  // the value of lane ^ 32
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -77,7 +81,10 @@ __device__ inline void to_lds(const void* base, uint32_t offset, uint32_t to) {
 __device__ inline void to_lds(const void* from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
 }
-__device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+template <int N>  // until at most the last N are under way
+__device__ inline void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
 __device__ inline void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 #define GRID_LDS __attribute__((address_space(3)))
@@ -89,59 +96,52 @@ __device__ constexpr int swz(int row) {
   return D == 64 ? ((row >> 1 & 1) << 2 | (row >> 2 & 3)) : ((row & 3) << 2 | (row >> 2 & 3));
 }
 
-// RW x KW waves: RW * 32 rows, stages of KW * KT keys of which a wave takes KT.  With one wave of rows a wave loads its
-// own keys and waits for nobody; otherwise the stage is shared.  DEPTH stages are held.  UNI: the rows that one load
-// instruction brings (64 / PR) lie in one page, so their address is a scalar and an offset that does not change.
-template <typename T, int D, int RW, int KW, int KT, int DEPTH, int WGS, bool UNI>
-__global__ __launch_bounds__(64 * RW * KW, RW * KW * WGS / 4) void tile_kernel(Paged P, AttendArgs a) {
-  typedef typename Vec<T>::eight Eight;
-  constexpr int W = RW * KW, NT = 64 * W, TM = 32 * RW, SK = KW * KT;
-  constexpr int PR = D / 8;               // 16-byte pieces of a row
-  constexpr int RPI = 64 / PR;            // rows that one load instruction brings
-  constexpr int LOADS = SK * PR / NT;     // of the keys, as many of the values, a thread
-  constexpr int KB = KT / 32, DB = D / 32, QS = D / 16;
-  constexpr bool PRIV = RW == 1;
-  constexpr uint32_t kHalf = SK * D * 2;  // bytes of a stage's keys
-  constexpr uint32_t kMerge = KW == 1 ? 0 : KW * TM * (2 + D / 2 + 4) * 4;  // what waves of other keys meet in
-  constexpr uint32_t kLds = DEPTH * 2 * kHalf > kMerge ? DEPTH * 2 * kHalf : kMerge;
-  static_assert(SK * PR % NT == 0 && 128 % SK == 0 && KT % RPI == 0, "");
-  __shared__ __attribute__((aligned(16))) uint8_t lds[kLds];
+// The keys whose values were cleaned: first, and after the last.
+__device__ inline void no_fix(int* fix) {
+  if (threadIdx.x == 0) {
+    fix[0] = INT32_MAX;
+    fix[1] = 0;
+  }
+}
 
+// RW x KW waves: RW * 32 rows, stages of KW * KT keys of which a wave takes KT.
+//  - RW == 1: a wave loads its own keys and waits for nobody.  One stage is held; the next keys are fetched when the
+//    scores have been computed, the next values when the sums have, so loads are in flight all the time.
+//  - RW > 1: the waves share the stages; two are held, the next one is fetched while one is worked on.
+// UNI: pages hold whole runs of 16 rows, so the address of a load is a scalar and an offset of the lane.
+template <typename T, int D_, int RW_, int KW_, int KT_, int WGS_, bool UNI_>
+struct Tile {
+  static constexpr int D = D_, RW = RW_, KW = KW_, KT = KT_, WGS = WGS_;
+  static constexpr bool UNI = UNI_, PRIV = RW == 1;
+  static constexpr int W = RW * KW, NT = 64 * W, TM = 32 * RW, SK = KW * KT;
+  static constexpr int PR = D / 8;            // 16-byte pieces of a row
+  static constexpr int RPI = 64 / PR;         // rows that one load instruction brings
+  static constexpr int WR = SK / W;           // rows that a wave brings: of the keys, as many of the values
+  static constexpr int LOADS = WR / RPI;      // load instructions for them
+  static constexpr int RUN = WR < 16 ? WR : 16, RUNS = WR / RUN;  // rows that share a page lookup
+  static constexpr int KB = KT / 32, DB = D / 32, QS = D / 16;
+  static constexpr uint32_t kHalf = SK * D * 2;  // bytes of a stage's keys
+  static constexpr uint32_t kStages = (PRIV ? 1 : 2) * 2 * kHalf;
+  static constexpr uint32_t kMerge = KW == 1 ? 0 : KW * TM * (2 + D / 2 + 4) * 4;  // what waves of other keys meet in
+  static constexpr uint32_t kLds = kStages > kMerge ? kStages : kMerge;
+  typedef typename Vec<T>::eight Eight;
+  static_assert(WR % RPI == 0 && 128 % SK == 0 && KT % 32 == 0, "");
+
+  // One sequence's key head, one tile of rows, the keys s_lo .. s_hi - 1 (s_lo a multiple of the stage).  whole: these
+  // are all the keys the rows see, the result is written; otherwise the sums go to slot `slot`.  fix: in LDS, no_fix()
+  // for all to see; so is it for the next call after a barrier and no_fix().
+  static __device__ __forceinline__ void run(const Paged& P, const AttendArgs& a, uint8_t* lds, int* fix, const Chunk& ch,
+                                             int b, int g, int tile, int s_lo, int s_hi, bool whole, int64_t slot);
+};
+
+template <typename T, int D_, int RW_, int KW_, int KT_, int WGS_, bool UNI_>
+__device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(const Paged& P, const AttendArgs& a,
+                                                                            uint8_t* lds, int* fix, const Chunk& ch,
+                                                                            int b, int g, int tile, int s_lo, int s_hi,
+                                                                            bool whole, int64_t slot) {
   const int tid = (int)threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rw = wave % RW, kw = wave / RW, half = lane >> 5, col = lane & 31;
-  // block -> (sequence, key head, tile, split)
-  uint32_t id = blockIdx.x;
-  const int split = (int)(id % (uint32_t)a.splits);
-  id /= (uint32_t)a.splits;
-  const int tile = a.tiles - 1 - (int)(id % (uint32_t)a.tiles);  // the longest first
-  id /= (uint32_t)a.tiles;
-  const int g = (int)(id % (uint32_t)P.hkv), b = (int)(id / (uint32_t)P.hkv);
-
-  const Chunk ch = chunk_of(P, b);
-  const int G = (int)a.group.d;
-  if (!ch.ok || ch.n > a.max_q || ch.kv > a.max_kv) {
-    // a bad sequence's rows: NaN, by its first block
-    if (split == 0 && tile == 0 && g == 0) {
-      const int from = min(max(ch.first, 0), P.T), to = min(max(P.cu_q[b + 1], from), P.T);
-      for (int64_t i = tid; i < (int64_t)(to - from) * a.hq * D; i += NT) {
-        const int t = from + (int)(i / (a.hq * D)), e = (int)(i % (a.hq * D));
-        ((T*)a.out)[t * a.os[0] + (e / D) * a.os[1] + e % D] = (T)NAN;
-        if (a.lse && e % D == 0) a.lse[(int64_t)t * a.hq + e / D] = NAN;
-      }
-    }
-    return;
-  }
-  const int rows = ch.n * G, first_pos = ch.kv - ch.n;
-  if (tile * TM >= rows) return;
-  // the keys of this block: those its rows see, within the split
-  const int start = split_start(a, ch);
-  const int last_i = min((int)a.group.quot((uint32_t)(tile * TM + TM - 1)), ch.n - 1);
-  const int first_i = (int)a.group.quot((uint32_t)(tile * TM));
-  const int lo_tile = a.window ? max(0, first_pos + first_i - a.window + 1) : 0;
-  const int s_lo = max(start + split * a.len, lo_tile) / SK * SK;
-  const int s_hi = (int)min((int64_t)start + (int64_t)(split + 1) * a.len, (int64_t)first_pos + last_i + 1);
-  if (s_lo >= s_hi) return;
-  const bool whole = ch.kv - start <= a.len;  // one split: the result, not a part of it
+  const int G = (int)a.group.d, rows = ch.n * G, first_pos = ch.kv - ch.n;
 
   // this wave's rows: lane's query, its position, the wave's range of positions
   const int r0 = tile * TM + rw * 32, r = min(r0 + col, rows - 1);
@@ -150,8 +150,53 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW * WGS / 4) void tile_kernel(P
   const int pos_min = first_pos + (int)a.group.quot((uint32_t)min(r0, rows - 1));
   const int pos_max = first_pos + (int)a.group.quot((uint32_t)min(r0 + 31, rows - 1));
 
+  // Loads.  Load i of a wave brings RPI rows from row WR * wave + i * RPI of the stage on, a lane piece `lane % PR` of
+  // row `lane / PR`; rows at and after s_hi are the last row again.
+  const uint32_t base = (uint32_t)(uintptr_t)(GRID_LDS uint8_t*)lds;
+  const uint16_t *kg = P.k + g * P.ks[2], *vg = P.v + g * P.vs[2];
+  const auto* table = (const __attribute__((address_space(4))) int32_t*)(P.table + (int64_t)b * P.table_stride);
+  const int lrow = lane / PR;
+  constexpr int FIND = UNI ? RUNS : LOADS;
+  int32_t page[FIND];
+  uint32_t row[FIND];
+  bool missing = false;
+  const auto find = [&](int s0) {
+#pragma unroll
+    for (int i = 0; i < FIND; ++i) {
+      const int s = s0 + wave * WR + (UNI ? i * RUN : i * RPI + lrow);
+      const uint32_t at = (uint32_t)(UNI ? min(s, (s_hi - 1) & ~(RUN - 1)) : min(s, s_hi - 1));
+      const uint32_t c = P.page.quot(at);
+      row[i] = at - c * P.page.d;
+      page[i] = table[c];
+    }
+#pragma unroll
+    for (int i = 0; i < FIND; ++i) {
+      const bool in = P.in_cache(page[i]);
+      missing |= !in;
+      page[i] = in ? page[i] : 0;
+    }
+  };
+  const auto fetch = [&](const uint16_t* x, const int64_t* st, int s0, uint32_t to) {
+    to += (uint32_t)(wave * WR * D * 2);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int piece = lane % PR ^ swz<D>(wave * WR + i * RPI + lrow);
+      if constexpr (UNI) {
+        constexpr int PER = RUN / RPI;
+        const int f = i / PER, s = s0 + wave * WR + f * RUN;
+        const uint16_t* p = x + (uint64_t)(uint32_t)page[f] * (uint32_t)st[0] + (uint64_t)row[f] * (uint32_t)st[1];
+        const int last = s_hi - 1 - min(s, (s_hi - 1) & ~(RUN - 1));  // last row of the run to read
+        const uint32_t rr = (uint32_t)min(i % PER * RPI + lrow, last);
+        to_lds(p, (rr * (uint32_t)st[1] + piece * 8) * 2, to + i * 1024);
+      } else {
+        to_lds(x + (uint64_t)(uint32_t)page[i] * (uint32_t)st[0] + (uint64_t)row[i] * (uint32_t)st[1] + piece * 8,
+               to + i * 1024);
+      }
+    }
+  };
+
   Eight q[QS];
-  {
+  const auto load_q = [&] {
     const uint16_t* src = a.q + qt * a.qs[0] + qh * a.qs[1] + half * 8;
     const uint32_t flip = a.negate ? 0x80008000u : 0u;
 #pragma unroll
@@ -160,53 +205,6 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW * WGS / 4) void tile_kernel(P
       x.x ^= flip, x.y ^= flip, x.z ^= flip, x.w ^= flip;
       q[k] = __builtin_bit_cast(Eight, x);
     }
-  }
-
-  // Stage rows: load i of a wave brings RPI rows from row_of(i) on, a lane piece `lane % PR` of row `lane / PR`.
-  const auto row_of = [&](int i) { return PRIV ? kw * KT + i * RPI : (i * W + wave) * RPI; };
-  const uint32_t base = (uint32_t)(uintptr_t)(GRID_LDS uint8_t*)lds;
-  const int lrow = lane / PR;
-  int32_t page[LOADS];
-  uint32_t row[LOADS];
-  bool missing = false;
-  const auto find = [&](int s0) {
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      if constexpr (UNI) {
-        const uint32_t s = (uint32_t)min(s0 + row_of(i), (s_hi - 1) / RPI * RPI);
-        const uint32_t c = P.page.quot(s);
-        row[i] = s - c * P.page.d;
-        page[i] = ((const __attribute__((address_space(4))) int32_t*)(P.table + (int64_t)b * P.table_stride))[c];
-      } else {
-        page[i] = P.page_of(b, (uint32_t)min(s0 + row_of(i) + lrow, s_hi - 1), row[i]);
-      }
-    }
-  };
-  const auto fetch = [&](int s0, int buf) {
-    if constexpr (PRIV) wait_reads();
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int rr = row_of(i) + lrow, piece = lane % PR ^ swz<D>(rr);
-      const bool in = P.in_cache(page[i]);
-      missing |= !in;
-      const uint32_t pg = in ? (uint32_t)page[i] : 0u;
-      const uint32_t to = base + (uint32_t)buf * 2 * kHalf + (uint32_t)row_of(i) * D * 2;
-      const uint16_t* k = P.k + (uint64_t)pg * (uint32_t)P.ks[0] + (uint64_t)row[i] * (uint32_t)P.ks[1] + g * P.ks[2];
-      const uint16_t* v = P.v + (uint64_t)pg * (uint32_t)P.vs[0] + (uint64_t)row[i] * (uint32_t)P.vs[1] + g * P.vs[2];
-      if constexpr (UNI) {
-        // rows at and after s_hi: the last row again
-        const uint32_t r = (uint32_t)min(lrow, s_hi - 1 - min(s0 + row_of(i), (s_hi - 1) / RPI * RPI));
-        to_lds(k, (r * (uint32_t)P.ks[1] + piece * 8) * 2, to);
-        to_lds(v, (r * (uint32_t)P.vs[1] + piece * 8) * 2, to + kHalf);
-      } else {
-        to_lds(k + piece * 8, to);
-        to_lds(v + piece * 8, to + kHalf);
-      }
-    }
-  };
-  const auto arrived = [&] {
-    wait_loads();
-    if constexpr (!PRIV) __syncthreads();
   };
 
   float16_v o[DB];
@@ -216,152 +214,202 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW * WGS / 4) void tile_kernel(P
     for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
   float m = -INFINITY, l = 0.f;
 
-  find(s_lo);
-  if constexpr (DEPTH > 1) {
-    fetch(s_lo, 0);
+  // S^T of the wave's keys
+  float16_v s[KB];
+  const auto scores = [&](const uint8_t* ks) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
+#pragma unroll
+      for (int k = 0; k < QS; ++k) {
+        const int piece = (2 * k + half) ^ swz<D>(col);
+        const Eight kk = *(const Eight*)(ks + (kb * 32 + col) * D * 2 + piece * 16);
+        s[kb] = Vec<T>::mfma(kk, q[k], s[kb]);
+      }
+    }
+  };
+  const auto mask = [&](int k0) {
+    const int hi = min(pos, s_hi - 1), lo = a.window ? pos - a.window : -1;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = k0 + kb * 32 + 8 * (i / 4) + 4 * half + i % 4;
+        s[kb][i] = key <= hi && key > lo ? s[kb][i] : -INFINITY;
+      }
+  };
+  // Values that are not finite must not meet a weight of 0 in a product.  In stages where some row does not see some
+  // key they are taken out, by the wave that loaded them, and added at the end to the rows that see them (settle).
+  const auto clean = [&](uint32_t at, int s0) {
+    uint4* mine = (uint4*)(lds + (at - base) + wave * WR * D * 2 + lane * 16);
+    uint32_t found = 0;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const uint4 x = mine[i * 64];
+      found |= (x.x & Vec<T>::kExp) + Vec<T>::kOne;
+      found |= (x.y & Vec<T>::kExp) + Vec<T>::kOne;
+      found |= (x.z & Vec<T>::kExp) + Vec<T>::kOne;
+      found |= (x.w & Vec<T>::kExp) + Vec<T>::kOne;
+    }
+    if (__any((found & 0x80008000u) != 0)) {
+      for (int i = 0; i < LOADS * 4; ++i) {
+        uint32_t* x = (uint32_t*)(mine + i / 4 * 64) + i % 4;
+        const uint32_t e = (*x & Vec<T>::kExp) + Vec<T>::kOne;
+        *x &= (e & 0x8000u ? 0u : 0xFFFFu) | (e & 0x80000000u ? 0u : 0xFFFF0000u);
+      }
+      if (lane == 0) {
+        atomicMin(&fix[0], s0 + wave * WR);
+        atomicMax(&fix[1], s0 + (wave + 1) * WR);
+      }
+    }
+  };
+  const auto masked = [&](int k0) {
+    return k0 + KT - 1 > pos_min || k0 + KT > s_hi || (a.window && k0 <= pos_max - a.window);
+  };
+  const auto softmax = [&] {
+    float top = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
+    top = fmaxf(top, other_half(top));
+    // The reference of the exponents follows the maximum only when it grows by more than 8 in base 2: weights stay
+    // below 2^8, and most stages need no rescaling.
+    if (__any(top > m && !((top - m) * a.c <= 8.f))) {
+      const float now = fmaxf(m, top), ref = now == -INFINITY ? 0.f : now;
+      const float keep = __builtin_amdgcn_exp2f((m - ref) * a.c);
+      l *= keep;
+#pragma unroll
+      for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] *= keep;
+      m = now;
+    }
+    const float mc = (m == -INFINITY ? 0.f : m) * a.c;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], a.c, -mc));
+        l += s[kb][i];
+      }
+  };
+  const auto sums = [&](const uint8_t* vs) {
+#pragma unroll
+    for (int t = 0; t < KT / 16; ++t) {
+      Eight p;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = (T)s[t / 2][t % 2 * 8 + i];
+#pragma unroll
+      for (int d = 0; d < DB; ++d) {
+        // V's operand: entry d * 32 + col of 8 keys, in the order the scores lie in
+        union {
+          short4_v four[2];
+          Eight all;
+        } v;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int l16 = lane & 15, rr = 16 * t + 8 * j + 4 * half + (l16 >> 2);
+          const int piece = (d * 4 + (lane >> 4 & 1) * 2 + (l16 >> 1 & 1)) ^ swz<D>(rr);
+          v.four[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (GRID_LDS short4_v*)(vs + rr * D * 2 + piece * 16 + (l16 & 1) * 8));
+        }
+        o[d] = Vec<T>::mfma(v.all, p, o[d]);
+      }
+    }
+  };
+
+  if constexpr (PRIV) {
+    const uint8_t *ks = lds + kw * KT * D * 2, *vs = ks + kHalf;
+    if (s_lo + kw * KT < s_hi) {
+      find(s_lo);
+      fetch(kg, P.ks, s_lo, base);
+      fetch(vg, P.vs, s_lo, base + kHalf);
+      load_q();
+    }
+    for (int s0 = s_lo; s0 + kw * KT < s_hi; s0 += SK) {
+      const int k0 = s0 + kw * KT;
+      const bool more = k0 + SK < s_hi, seen = k0 <= pos_max && (!a.window || k0 + KT > pos_min - a.window + 1);
+      if (more) find(s0 + SK);
+      wait_loads<LOADS>();
+      if (seen) scores(ks);
+      wait_reads();
+      if (more) {
+        fetch(kg, P.ks, s0 + SK, base);
+        wait_loads<LOADS>();
+      } else {
+        wait_loads<0>();
+      }
+      if (seen) {
+        if (masked(k0)) {
+          mask(k0);
+          clean(base + kHalf, s0);
+        }
+        softmax();
+        sums(vs);
+      }
+      wait_reads();
+      if (more) fetch(vg, P.vs, s0 + SK, base + kHalf);
+    }
+  } else {
+    find(s_lo);
+    fetch(kg, P.ks, s_lo, base);
+    fetch(vg, P.vs, s_lo, base + kHalf);
+    load_q();
     if (s_lo + SK < s_hi) find(s_lo + SK);
-    arrived();
-  }
-  int buf = 0;
-  for (int s0 = s_lo; s0 < s_hi; s0 += SK, buf ^= DEPTH - 1) {
-    if constexpr (DEPTH > 1) {
+    // stages that some row of the tile does not see all of
+    const int tile_min = first_pos + (int)a.group.quot((uint32_t)(tile * TM));
+    const int tile_max = first_pos + (int)a.group.quot((uint32_t)min(tile * TM + TM, rows) - 1u);
+    const auto torn = [&](int s0) {
+      return s0 + SK - 1 > tile_min || s0 + SK > s_hi || (a.window && s0 <= tile_max - a.window);
+    };
+    wait_loads<0>();
+    if (torn(s_lo)) clean(base + kHalf, s_lo);
+    __syncthreads();
+    uint32_t buf = 0;
+    for (int s0 = s_lo; s0 < s_hi; s0 += SK) {
       if (s0 + SK < s_hi) {
-        fetch(s0 + SK, buf ^ 1);
+        fetch(kg, P.ks, s0 + SK, base + (buf ^ 2 * kHalf));
+        fetch(vg, P.vs, s0 + SK, base + (buf ^ 2 * kHalf) + kHalf);
         if (s0 + 2 * SK < s_hi) find(s0 + 2 * SK);
       }
-    } else {
-      fetch(s0, 0);
-      if (s0 + SK < s_hi) find(s0 + SK);
-      arrived();
-    }
-    const int k0 = s0 + kw * KT;  // this wave's keys
-    const bool work = alive && k0 <= pos_max && k0 < s_hi && (!a.window || k0 + KT > pos_min - a.window + 1);
-    if (work) {
-      const uint8_t* ks = lds + buf * 2 * kHalf + kw * KT * D * 2;
-      const uint8_t* vs = ks + kHalf;
-      float16_v s[KB];
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
-#pragma unroll
-        for (int k = 0; k < QS; ++k) {
-          const int piece = (2 * k + half) ^ swz<D>(col);
-          const Eight kk = *(const Eight*)(ks + (kb * 32 + col) * D * 2 + piece * 16);
-          s[kb] = Vec<T>::mfma(kk, q[k], s[kb]);
-        }
+      const int k0 = s0 + kw * KT;
+      if (alive && k0 < s_hi && k0 <= pos_max && (!a.window || k0 + KT > pos_min - a.window + 1)) {
+        const uint8_t *ks = lds + buf + kw * KT * D * 2, *vs = ks + kHalf;
+        scores(ks);
+        if (masked(k0)) mask(k0);
+        softmax();
+        sums(vs);
       }
-      const bool masked = k0 + KT - 1 > pos_min || k0 + KT > s_hi || (a.window && k0 <= pos_max - a.window);
-      bool poison = false;
-      if (masked) {
-        const int hi = min(pos, s_hi - 1), lo = a.window ? pos - a.window : -1;
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int key = k0 + kb * 32 + 8 * (i / 4) + 4 * half + i % 4;
-            s[kb][i] = key <= hi && key > lo ? s[kb][i] : -INFINITY;
-          }
-        // values that are not finite must not meet a weight of 0 in a product
-        uint32_t found = 0;
-#pragma unroll
-        for (int i = 0; i < KT * D * 2 / 1024; ++i) {
-          const uint4 x = *(const uint4*)(vs + i * 1024 + lane * 16);
-          found |= (x.x & Vec<T>::kExp) + Vec<T>::kOne;
-          found |= (x.y & Vec<T>::kExp) + Vec<T>::kOne;
-          found |= (x.z & Vec<T>::kExp) + Vec<T>::kOne;
-          found |= (x.w & Vec<T>::kExp) + Vec<T>::kOne;
-        }
-        poison = __any((found & 0x80008000u) != 0);
-      }
-      float top = s[0][0];
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
-      top = fmaxf(top, other_half(top));
-      // The reference of the exponents follows the maximum only when it grows by more than 8 in base 2: weights stay
-      // below 2^8, and most stages need no rescaling.
-      if (__any(top > m && !((top - m) * a.c <= 8.f))) {
-        const float now = fmaxf(m, top), ref = now == -INFINITY ? 0.f : now;
-        const float keep = __builtin_amdgcn_exp2f((m - ref) * a.c);
-        l *= keep;
-#pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[d][i] *= keep;
-        m = now;
-      }
-      const float mc = (m == -INFINITY ? 0.f : m) * a.c;
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[kb][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][i], a.c, -mc));
-          l += s[kb][i];
-        }
-      auto product = [&](auto clean) {
-#pragma unroll
-        for (int t = 0; t < KT / 16; ++t) {
-          Eight p;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) p[i] = (T)s[t / 2][t % 2 * 8 + i];
-#pragma unroll
-          for (int d = 0; d < DB; ++d) {
-            union {
-              short4_v four[2];
-              uint32_t pair[4];
-              Eight all;
-            } v;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const int l16 = lane & 15, rr = 16 * t + 8 * j + 4 * half + (l16 >> 2);
-              const int piece = (d * 4 + (lane >> 4 & 1) * 2 + (l16 >> 1 & 1)) ^ swz<D>(rr);
-              v.four[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                  (GRID_LDS short4_v*)(vs + rr * D * 2 + piece * 16 + (l16 & 1) * 8));
-            }
-            if constexpr (clean())
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const uint32_t e = (v.pair[j] & Vec<T>::kExp) + Vec<T>::kOne;
-                v.pair[j] &= (e & 0x8000u ? 0u : 0xFFFFu) | (e & 0x80000000u ? 0u : 0xFFFF0000u);
-              }
-            o[d] = Vec<T>::mfma(v.all, p, o[d]);
-          }
-        }
-      };
-      if (!poison) {
-        product(std::false_type());
-      } else {
-        // the finite values as ever; then the others, one by one, where their weight is above 0
-        product(std::true_type());
-        for (int kk = 0; kk < KT; ++kk) {
-          const int reg = kk / 32 * 16 + (kk >> 3 & 3) * 4 + (kk & 3);
-          float p = 0.f;
-#pragma unroll
-          for (int i = 0; i < KB * 16; ++i) p = i == reg ? s[i / 16][i % 16] : p;
-          p = (float)(T)__shfl(p, col + (kk & 4) * 8);
-          const uint16_t* vr = (const uint16_t*)(vs + kk * D * 2);
-#pragma unroll
-          for (int d = 0; d < DB; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int e = d * 32 + 8 * (i / 4) + 4 * half + i % 4;
-              const uint16_t v = vr[(e / 8 ^ swz<D>(kk)) * 8 + e % 8];
-              if ((v & Vec<T>::kExp) + Vec<T>::kOne & 0x8000u && p > 0.f) o[d][i] += p * (float)__builtin_bit_cast(T, v);
-            }
-        }
-      }
-    }
-    if constexpr (DEPTH > 1)
-      arrived();
-    else if constexpr (!PRIV)
+      buf ^= 2 * kHalf;
+      wait_loads<0>();
+      if (s0 + SK < s_hi && torn(s0 + SK)) clean(base + buf + kHalf, s0 + SK);
       __syncthreads();
+    }
   }
   l += other_half(l);
   missing = __syncthreads_or(missing);
   if (missing) l = NAN;
   float mc = m * a.c;  // -inf where the row saw nothing
+
+  // adds to four sums of the row at position p the values that were taken out and that it sees
+  const int fix_lo = fix[0], fix_hi = min(fix[1], s_hi);
+  const auto settle = [&](float4& x, int p, int e) {
+    if (fix_lo >= fix_hi) return;
+    for (int s = max(fix_lo, a.window ? p - a.window + 1 : 0); s < min(fix_hi, p + 1); ++s) {
+      uint32_t rr;
+      const int id = P.page_of(b, (uint32_t)s, rr);
+      if (!P.in_cache(id)) continue;
+      T y[4];
+      __builtin_memcpy(y, vg + (uint64_t)(uint32_t)id * (uint32_t)P.vs[0] + (uint64_t)rr * (uint32_t)P.vs[1] + e, 8);
+      const float f[4] = {(float)y[0], (float)y[1], (float)y[2], (float)y[3]};
+      x.x += __builtin_isfinite(f[0]) ? 0.f : f[0];
+      x.y += __builtin_isfinite(f[1]) ? 0.f : f[1];
+      x.z += __builtin_isfinite(f[2]) ? 0.f : f[2];
+      x.w += __builtin_isfinite(f[3]) ? 0.f : f[3];
+    }
+  };
 
   // waves that took other keys of the same rows: their sums meet in LDS
   if constexpr (KW > 1) {
@@ -414,15 +462,15 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW * WGS / 4) void tile_kernel(P
         }
         const int i = (int)a.group.quot((uint32_t)(tile * TM + rr)), h = g * G + tile * TM + rr - i * G, t = ch.first + i;
         const float rm = ml[rr], rl = ml[TM + rr];
+        settle(x, first_pos + i, hd * DH + e);
         if (whole) {
           const float over = rl == 0.f ? 0.f : 1.f / rl;
           T y[4] = {(T)(x.x * over), (T)(x.y * over), (T)(x.z * over), (T)(x.w * over)};
           *(uint2*)(a.out + t * a.os[0] + h * a.os[1] + hd * DH + e) = *(uint2*)y;
           if (a.lse && e == 0 && hd == 0) a.lse[(int64_t)t * a.hq + h] = (rm + __builtin_amdgcn_logf(rl)) * kLn2;
         } else {
-          const int64_t slot = ((int64_t)split * P.T + t) * a.hq + h;
-          *(float4*)(a.part_o + slot * D + hd * DH + e) = x;
-          if (e == 0 && hd == 0) a.part_ml[slot] = make_float2(rm, rl);
+          *(float4*)(a.part_o + (slot * TM + rr) * D + hd * DH + e) = x;
+          if (e == 0 && hd == 0) a.part_ml[slot * TM + rr] = make_float2(rm, rl);
         }
       }
       if (hd == 0) __syncthreads();
@@ -436,25 +484,153 @@ __global__ __launch_bounds__(64 * RW * KW, RW * KW * WGS / 4) void tile_kernel(P
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
-          T y[4] = {(T)(o[d][i] * over), (T)(o[d][i + 1] * over), (T)(o[d][i + 2] * over), (T)(o[d][i + 3] * over)};
+          float4 x = make_float4(o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]);
+          settle(x, pos, d * 32 + 2 * i + 4 * half);
+          T y[4] = {(T)(x.x * over), (T)(x.y * over), (T)(x.z * over), (T)(x.w * over)};
           *(uint2*)(dst + d * 32 + 2 * i) = *(uint2*)y;
         }
       if (a.lse && half == 0) a.lse[(int64_t)qt * a.hq + qh] = (mc + __builtin_amdgcn_logf(l)) * kLn2;
     } else {
-      const int64_t slot = ((int64_t)split * P.T + qt) * a.hq + qh;
-      float* dst = a.part_o + slot * D + 4 * half;
+      const int64_t at = slot * TM + rw * 32 + col;
+      float* dst = a.part_o + at * D + 4 * half;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; i += 4)
-          *(float4*)(dst + d * 32 + 2 * i) = make_float4(o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]);
-      if (half == 0) a.part_ml[slot] = make_float2(mc, l);
+          {
+          float4 x = make_float4(o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]);
+          settle(x, pos, d * 32 + 2 * i + 4 * half);
+          *(float4*)(dst + d * 32 + 2 * i) = x;
+          }
+      if (half == 0) a.part_ml[at] = make_float2(mc, l);
     }
   }
 }
 
-// The splits of a row joined: a workgroup a token and head, D / 4 lanes a split, several splits side by side.
+// The rows of a bad sequence.
 template <typename T, int D>
+__device__ void fill_nan(const Paged& P, const AttendArgs& a, const Chunk& ch, int b, int nt) {
+  const int from = min(max(ch.first, 0), P.T), to = min(max(P.cu_q[b + 1], from), P.T);
+  for (int64_t i = threadIdx.x; i < (int64_t)(to - from) * a.hq * D; i += nt) {
+    const int t = from + (int)(i / (a.hq * D)), e = (int)(i % (a.hq * D));
+    ((T*)a.out)[t * a.os[0] + (e / D) * a.os[1] + e % D] = (T)NAN;
+    if (a.lse && e % D == 0) a.lse[(int64_t)t * a.hq + e / D] = NAN;
+  }
+}
+
+// Many rows: a workgroup a tile of rows of one sequence and key head and one of `splits` ranges of keys.
+template <typename T, typename X>
+__global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void tiles_kernel(Paged P, AttendArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t lds[X::kLds];
+  __shared__ int fix[2];
+  no_fix(fix);
+  __syncthreads();
+  uint32_t id = blockIdx.x;
+  const int split = (int)(id % (uint32_t)a.splits);
+  id /= (uint32_t)a.splits;
+  const int tile = a.tiles - 1 - (int)(id % (uint32_t)a.tiles);  // the longest first
+  id /= (uint32_t)a.tiles;
+  const int g = (int)(id % (uint32_t)P.hkv), b = (int)(id / (uint32_t)P.hkv);
+  const Chunk ch = chunk_of(P, b);
+  if (is_bad(a, ch)) {
+    if (split == 0 && tile == 0 && g == 0) fill_nan<T, X::D>(P, a, ch, b, X::NT);
+    return;
+  }
+  if (tile * X::TM >= ch.n * (int)a.group.d) return;
+  // the keys that the tile's rows see, within the range
+  const int start = first_key(a, ch), first_pos = ch.kv - ch.n;
+  const int first_i = (int)a.group.quot((uint32_t)(tile * X::TM));
+  const int last_i = min((int)a.group.quot((uint32_t)(tile * X::TM + X::TM - 1)), ch.n - 1);
+  const int seen = a.window ? max(0, first_pos + first_i - a.window + 1) : 0;
+  const int s_lo = max(start + split * a.len, seen) / X::SK * X::SK;
+  const int s_hi = (int)min((int64_t)start + (int64_t)(split + 1) * a.len, (int64_t)first_pos + last_i + 1);
+  if (s_lo >= s_hi) return;
+  X::run(P, a, lds, fix, ch, b, g, tile, s_lo, s_hi, ch.kv - start <= a.len,
+         (((int64_t)b * P.hkv + g) * a.tiles + tile) * a.splits + split);
+}
+
+// Few rows: every sequence's rows are one tile, and the work is the stages of all sequences and key heads in a row,
+// cut into equal shares: workgroup i takes stages i * total / n .. (i + 1) * total / n - 1, whatever units they belong
+// to.  So all finish together, however ragged the lengths.  Of a unit that workgroups share, the sums of the one that
+// begins it go to its slot 2 i + 1, those of the others to 2 i; runs tells the joining kernel which they are.
+template <typename T, typename X>
+__global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void shares_kernel(Paged P, AttendArgs a) {
+  __shared__ __attribute__((aligned(16))) uint8_t lds[X::kLds];
+  __shared__ uint64_t waves[X::W], found[2];
+  __shared__ int fix[2];
+  no_fix(fix);
+  const int tid = (int)threadIdx.x, lane = tid & 63;
+  const uint64_t me = blockIdx.x, heads = (uint64_t)P.hkv;
+  const auto stages = [&](const Chunk& c) {
+    return is_bad(a, c) || c.n == 0 ? 0u : (uint32_t)((c.kv - first_key(a, c) + X::SK - 1) / X::SK);
+  };
+  // stages of the sequences before a thread's: each thread adds up a run of sequences
+  const int per = (P.B + X::NT - 1) / X::NT, b0 = min(tid * per, P.B), b1 = min(b0 + per, P.B);
+  uint64_t mine = 0;
+  for (int b = b0; b < b1; ++b) mine += stages(chunk_of(P, b));
+  uint64_t upto = mine;
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint64_t x = __shfl_up((unsigned long long)upto, o);
+    if (lane >= o) upto += x;
+  }
+  if (lane == 63) waves[tid >> 6] = upto;
+  __syncthreads();
+  uint64_t total = 0;
+  for (int w = 0; w < X::W; ++w) {
+    if (w < tid >> 6) upto += waves[w];
+    total += waves[w];
+  }
+  total *= heads;
+  for (int b = (int)me; b < P.B; b += (int)gridDim.x) {
+    const Chunk c = chunk_of(P, b);
+    if (is_bad(a, c)) fill_nan<T, X::D>(P, a, c, b, X::NT);
+  }
+  const uint64_t n = min((uint64_t)gridDim.x, total);  // no share is empty
+  if (me >= n) return;
+  uint64_t x = me * total / n;
+  const uint64_t end = (me + 1) * total / n;
+  if (x >= (upto - mine) * heads && x < upto * heads) {
+    uint64_t before = upto - mine;
+    int b = b0;
+    for (; b < b1 - 1; ++b) {
+      const uint32_t s = stages(chunk_of(P, b));
+      if (x < (before + s) * heads) break;
+      before += s;
+    }
+    found[0] = (uint64_t)b;
+    found[1] = before;
+  }
+  __syncthreads();
+  int b = (int)found[0];
+  uint64_t first = found[1] * heads;  // stages before sequence b
+  b = __builtin_amdgcn_readfirstlane(b);
+  while (x < end) {
+    const Chunk ch = chunk_of(P, b);
+    const uint64_t s = stages(ch);
+    if (x >= first + s * heads) {  // the next sequence (b < P.B: x < end <= total)
+      first += s * heads;
+      ++b;
+      continue;
+    }
+    const int g = __builtin_amdgcn_readfirstlane((int)((uint32_t)(x - first) / (uint32_t)s));
+    const uint64_t unit = first + (uint64_t)g * s, stop = min(end, unit + s);
+    const bool whole = x == unit && stop == unit + s;
+    if (x == unit && tid == 0)
+      a.runs[(int64_t)b * P.hkv + g] = make_int2((int)me, (int)(((unit + s) * n - 1) / total));
+    const int start = first_key(a, ch);
+    const int s_lo = __builtin_amdgcn_readfirstlane(start + (int)(x - unit) * X::SK);
+    const int s_hi = __builtin_amdgcn_readfirstlane(min(ch.kv, start + (int)(stop - unit) * X::SK));
+    X::run(P, a, lds, fix, ch, b, g, 0, s_lo, s_hi, whole, (int64_t)me * 2 + (x == unit));
+    x = stop;
+    if (x >= end) break;
+    __syncthreads();
+    no_fix(fix);
+    __syncthreads();
+  }
+}
+
+// The parts of a row joined: a workgroup a token and head, D / 4 lanes a part, several parts side by side.
+template <typename T, int D, int TM, bool SHARES>
 __global__ __launch_bounds__(256) void join_kernel(Paged P, AttendArgs a) {
   constexpr int L = D / 4, N = 256 / L;
   const int tid = (int)threadIdx.x, lane = tid & 63, e = tid % L * 4, side = tid / L;
@@ -463,11 +639,22 @@ __global__ __launch_bounds__(256) void join_kernel(Paged P, AttendArgs a) {
   for (int s = 0; s < P.B; s += 64) b += __popcll(__ballot(s + lane < P.B && P.cu_q[s + lane + 1] <= t));
   if (b >= P.B) return;
   const Chunk ch = chunk_of(P, b);
-  if (!ch.ok || ch.n > a.max_q || ch.kv > a.max_kv || t < ch.first || t >= ch.first + ch.n) return;
-  const int start = split_start(a, ch);
-  if (ch.kv - start <= a.len) return;
-  const int pos = ch.kv - ch.n + t - ch.first;
-  const int from = (max(a.window ? pos - a.window + 1 : 0, start) - start) / a.len, to = (pos - start) / a.len;
+  if (is_bad(a, ch) || t < ch.first || t >= ch.first + ch.n) return;
+  const int G = (int)a.group.d, g = (int)a.group.quot((uint32_t)h), r = (t - ch.first) * G + h - g * G;
+  int from, to;
+  int64_t slots = 0;
+  if constexpr (SHARES) {
+    const int2 run = a.runs[(int64_t)b * P.hkv + g];
+    from = run.x;
+    to = run.y;
+    if (from == to) return;
+  } else {
+    const int start = first_key(a, ch), pos = ch.kv - ch.n + t - ch.first;
+    if (ch.kv - start <= a.len) return;
+    from = (max(a.window ? pos - a.window + 1 : 0, start) - start) / a.len;
+    to = (pos - start) / a.len;
+    slots = (((int64_t)b * P.hkv + g) * a.tiles + r / TM) * a.splits;
+  }
   float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   const auto take = [&](float om, float ol, float4 x) {
@@ -480,9 +667,9 @@ __global__ __launch_bounds__(256) void join_kernel(Paged P, AttendArgs a) {
   };
 #pragma unroll 4
   for (int s = from + side; s <= to; s += N) {
-    const int64_t slot = ((int64_t)s * P.T + t) * a.hq + h;
-    const float2 p = a.part_ml[slot];
-    take(p.x, p.y, *(const float4*)(a.part_o + slot * D + e));
+    const int64_t at = (SHARES ? (int64_t)s * 2 + (s == from) : slots + s) * TM + r % TM;
+    const float2 p = a.part_ml[at];
+    take(p.x, p.y, *(const float4*)(a.part_o + at * D + e));
   }
   __shared__ float2 ml[N];
   __shared__ float4 os[N][L];
@@ -491,7 +678,7 @@ __global__ __launch_bounds__(256) void join_kernel(Paged P, AttendArgs a) {
   __syncthreads();
   if (side > 0) return;
 #pragma unroll
-  for (int n = 1; n < N; ++n) take(ml[n].x, ml[n].y, os[n][tid]);
+  for (int i = 1; i < N; ++i) take(ml[i].x, ml[i].y, os[i][tid]);
   const float over = l == 0.f ? 0.f : 1.f / l;
   T y[4] = {(T)(o.x * over), (T)(o.y * over), (T)(o.z * over), (T)(o.w * over)};
   *(uint2*)(a.out + t * a.os[0] + h * a.os[1] + e) = *(uint2*)y;
@@ -517,59 +704,88 @@ int check(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_a
 }
 
 
-// Rows of a tile, and the ranges of keys: with few tiles the keys are split until there are about 4096 workgroups,
-// none with fewer than 256 keys.
+// The launch.  Few rows (up to 64 a sequence and key head at most): tiles of 32 or 64 and equal shares of the stages,
+// two workgroups a compute unit, or fewer where there are fewer stages.  Many rows: tiles of 128; where they are fewer than
+// two workgroups a compute unit the keys are split, into ranges of at least 512.
+constexpr int kComputeUnits = 256;
 struct Shape {
   int tm, splits, len;
   int64_t tiles, blocks;
+  bool join;
+  size_t slots;  // of parts
 };
 Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_attend_args* g) {
   Shape s;
   const int group = g->n_heads / c->n_kv_heads;
   const int64_t rows = (int64_t)std::min(g->max_q, std::max(1, x->n_tokens)) * group;
-  s.tm = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
-  s.tiles = (rows + s.tm - 1) / s.tm;
-  const int64_t units = s.tiles * c->n_kv_heads * x->n_seqs;
   int64_t span = std::min<int64_t>(g->max_kv, (int64_t)x->table_cols * c->page_size);
   if (g->window) span = std::min<int64_t>(span, (int64_t)g->window + g->max_q + 127);
-  s.len = (int)std::min<int64_t>(std::max<int64_t>(256, (span * units / 1024 + 127) / 128 * 128), 32 * s.tm);
-  s.splits = (int)((span + s.len - 1) / s.len);
-  s.blocks = units * s.splits;
+  const int64_t heads = (int64_t)c->n_kv_heads * x->n_seqs;
+  s.tm = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  s.tiles = (rows + s.tm - 1) / s.tm;
+  s.splits = 1;
+  s.len = INT32_MAX;
+  if (s.tm < 128) {
+    const int64_t stage = 64, stages = (span + stage - 1) / stage;
+    s.blocks = std::min<int64_t>(heads * stages, 2 * kComputeUnits);
+    s.join = stages > 1;
+    s.slots = (size_t)s.blocks * 2;
+    return s;
+  }
+  s.blocks = heads * s.tiles;
+  // a joining workgroup a row has to fit a launch
+  if (s.blocks < 2 * kComputeUnits && (int64_t)x->n_tokens * g->n_heads <= 1 << 22) {
+    const int64_t len = (std::max<int64_t>(512, span * s.blocks / (4 * kComputeUnits)) + 127) / 128 * 128;
+    if (len < span) {
+      s.len = (int)len;
+      s.splits = (int)((span + len - 1) / len);
+      s.blocks *= s.splits;
+    }
+  }
+  s.join = s.splits > 1;
+  s.slots = s.join ? (size_t)s.blocks : 0;
   return s;
 }
 
-size_t workspace_of(const grid_paged_cache* c, const grid_chunks* x, const grid_attend_args* g, const Shape& s) {
-  if (s.splits <= 1) return 16;
-  return (size_t)s.splits * (size_t)x->n_tokens * (size_t)g->n_heads * (size_t)(c->head_dim + 2) * 4;
+size_t runs_bytes(const grid_paged_cache* c, const grid_chunks* x) {
+  return ((size_t)x->n_seqs * (size_t)c->n_kv_heads * sizeof(int2) + 15) / 16 * 16;
+}
+size_t workspace_of(const grid_paged_cache* c, const grid_chunks* x, const Shape& s) {
+  return runs_bytes(c, x) + s.slots * (size_t)s.tm * (size_t)(c->head_dim + 2) * 4;
 }
 
-template <typename T, int D, int RW, int KW, int KT, int DEPTH, int WGS>
+template <typename T, int D, int RW, int KW, int KT, int WGS>
 void launch(const Paged& P, const AttendArgs& a, const Shape& s, hipStream_t stream) {
-  const dim3 blocks((unsigned)s.blocks), threads(64 * RW * KW);
-  if (P.page.d % (512 / D) == 0)
-    hipLaunchKernelGGL((tile_kernel<T, D, RW, KW, KT, DEPTH, WGS, true>), blocks, threads, 0, stream, P, a);
+  const dim3 blocks((unsigned)s.blocks), rows((unsigned)P.T * (unsigned)a.hq);
+  constexpr bool SHARES = RW * 32 < 128;
+  const auto go = [&](auto tile) {
+    using X = decltype(tile);
+    if constexpr (SHARES)
+      hipLaunchKernelGGL((shares_kernel<T, X>), blocks, dim3(X::NT), 0, stream, P, a);
+    else
+      hipLaunchKernelGGL((tiles_kernel<T, X>), blocks, dim3(X::NT), 0, stream, P, a);
+  };
+  if (P.page.d % 16 == 0)
+    go(Tile<T, D, RW, KW, KT, WGS, true>());
   else
-    hipLaunchKernelGGL((tile_kernel<T, D, RW, KW, KT, DEPTH, WGS, false>), blocks, threads, 0, stream, P, a);
-  if (s.splits > 1) {
-    const dim3 rows((unsigned)P.T * (unsigned)a.hq);
-    hipLaunchKernelGGL((join_kernel<T, D>), rows, dim3(256), 0, stream, P, a);
-  }
+    go(Tile<T, D, RW, KW, KT, WGS, false>());
+  if (s.join) hipLaunchKernelGGL((join_kernel<T, D, RW * 32, SHARES>), rows, dim3(256), 0, stream, P, a);
 }
 
 template <typename T>
 void choose(const Paged& P, const AttendArgs& a, const Shape& s, hipStream_t stream) {
   if (P.D == 64)
-    s.tm == 32   ? launch<T, 64, 1, 4, 32, 1, 2>(P, a, s, stream)
-    : s.tm == 64 ? launch<T, 64, 2, 2, 32, 1, 2>(P, a, s, stream)
-                 : launch<T, 64, 4, 1, 64, 2, 2>(P, a, s, stream);
+    s.tm == 32   ? launch<T, 64, 1, 4, 32, 2>(P, a, s, stream)
+    : s.tm == 64 ? launch<T, 64, 2, 2, 32, 2>(P, a, s, stream)
+                 : launch<T, 64, 4, 1, 64, 2>(P, a, s, stream);
   else if (P.D == 128)
-    s.tm == 32   ? launch<T, 128, 1, 4, 32, 1, 2>(P, a, s, stream)
-    : s.tm == 64 ? launch<T, 128, 2, 2, 32, 1, 2>(P, a, s, stream)
-                 : launch<T, 128, 4, 1, 64, 2, 2>(P, a, s, stream);
+    s.tm == 32   ? launch<T, 128, 1, 4, 32, 2>(P, a, s, stream)
+    : s.tm == 64 ? launch<T, 128, 2, 2, 32, 2>(P, a, s, stream)
+                 : launch<T, 128, 4, 1, 64, 2>(P, a, s, stream);
   else
-    s.tm == 32   ? launch<T, 256, 1, 4, 32, 1, 1>(P, a, s, stream)
-    : s.tm == 64 ? launch<T, 256, 2, 2, 32, 1, 1>(P, a, s, stream)
-                 : launch<T, 256, 4, 1, 32, 2, 1>(P, a, s, stream);
+    s.tm == 32   ? launch<T, 256, 1, 4, 32, 1>(P, a, s, stream)
+    : s.tm == 64 ? launch<T, 256, 2, 2, 32, 1>(P, a, s, stream)
+                 : launch<T, 256, 4, 1, 32, 1>(P, a, s, stream);
 }
 
 }  // namespace
@@ -577,7 +793,7 @@ void choose(const Paged& P, const AttendArgs& a, const Shape& s, hipStream_t str
 extern "C" size_t grid_attend_workspace_bytes(const grid_paged_cache* cache, const grid_chunks* chunks,
                                               const grid_attend_args* args) {
   if (check(cache, chunks, args, false) != GRID_OK) return 0;
-  return workspace_of(cache, chunks, args, shape_of(cache, chunks, args));
+  return workspace_of(cache, chunks, shape_of(cache, chunks, args));
 }
 
 extern "C" int grid_attend(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_attend_args* args,
@@ -588,9 +804,10 @@ extern "C" int grid_attend(const grid_paged_cache* cache, const grid_chunks* chu
   if (chunks->n_tokens == 0) return GRID_OK;
   const Shape s = shape_of(cache, chunks, args);
   if (!args->workspace || (uintptr_t)args->workspace % 16 != 0 ||
-      args->workspace_bytes < workspace_of(cache, chunks, args, s))
+      args->workspace_bytes < workspace_of(cache, chunks, s))
     return fail(GRID_E_ARG, "grid_attend: workspace too small or not aligned");
-  if (s.blocks > (int64_t)1 << 23) return fail(GRID_E_CAPACITY, "grid_attend: too many tiles for one launch");
+  if (s.blocks > (int64_t)1 << 23 || (s.join && (int64_t)chunks->n_tokens * args->n_heads > (int64_t)1 << 23))
+    return fail(GRID_E_CAPACITY, "grid_attend: too many rows for one launch");
   AttendArgs a;
   a.q = (const uint16_t*)args->q;
   a.out = (uint16_t*)args->out;
@@ -599,8 +816,9 @@ extern "C" int grid_attend(const grid_paged_cache* cache, const grid_chunks* chu
     a.os[i] = args->out_stride[i];
   }
   a.lse = args->lse;
-  a.part_o = (float*)args->workspace;
-  a.part_ml = (float2*)(a.part_o + (size_t)s.splits * chunks->n_tokens * args->n_heads * cache->head_dim);
+  a.runs = (int2*)args->workspace;
+  a.part_o = (float*)((uint8_t*)args->workspace + runs_bytes(cache, chunks));
+  a.part_ml = (float2*)(a.part_o + s.slots * (size_t)s.tm * (size_t)cache->head_dim);
   a.group = Divisor((uint32_t)(args->n_heads / cache->n_kv_heads));
   a.hq = args->n_heads;
   a.max_q = args->max_q;
