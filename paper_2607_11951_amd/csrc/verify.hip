@@ -1,12 +1,16 @@
 // verify.hip -- grid_verify: drafted tokens against the target's masked distribution (gfx950).
 //
-// Two launches.  The first reads every row once, in slices, and leaves per slice the largest allowed logit m and
-// z = sum exp((l - m) / T), taken online.  The second joins a sequence's rows, finds the first refused draft and races
-// that one row's weights over the given noise: the argmax of w / noise needs no normaliser and no order, so the row is
-// split over workgroups whose best meet in an integer maximum (score bits, then the complement of the index: the
-// lowest index on ties, whatever the order).  The last workgroup of a sequence writes its outputs.
+// Two launches.  The first goes over the rows once: a workgroup takes a piece (some thousand tokens) of a row after the other, with the noise
+// of these tokens in registers, and leaves of each the largest allowed logit m, z = sum exp((l - m) / T), and the best of
+// the race exp((l - m) / T) / noise: an argmax that needs no normaliser and no order.  Logits are read only where the
+// mask allows one of a thread's 8 tokens.  The second joins a sequence's rows and finds the first refused draft.  Where
+// drafts come without probabilities, what is left of p after a refusal is p without the draft, so the first pass has
+// raced it already.  Otherwise max(p - q, 0) of that one row is raced by several workgroups, whose best meet in an integer
+// maximum (score bits, then the complement of the index: the lowest index on ties, whatever the order); the last of them
+// writes the sequence's outputs.
 #include <algorithm>
 #include <string>
+#include <type_traits>
 
 #include "paged.h"
 
@@ -15,10 +19,14 @@ using namespace grid;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kStep = kThreads * 8;  // tokens a workgroup takes a step: 8 a thread, one byte of mask
-constexpr int kMaxSlices = 64;       // of a row: a wave joins them
+constexpr int kWaves = kThreads / 64;
+template <typename T>                    // steps of 512 tokens, 8 a lane, that a wave takes of a row: 16-bit rows have
+constexpr int kSteps = 8 / sizeof(T);    // the longer ones, for the same registers
+constexpr int kPiece = kWaves * 512;     // tokens of a workgroup's piece, for each step
+constexpr int kStep = kThreads * 8;      // tokens that a workgroup of the residual's race takes a step
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLow = -3.402823466e38f;
+constexpr int kNone = 0x7FFFFFFF;
 
 struct VerifyArgs {
   const void* logits;
@@ -28,10 +36,10 @@ struct VerifyArgs {
   int64_t ls[2], ms[2], ps[2], ns;
   int32_t *tokens, *accepted;
   float* logprobs;
-  float4* part;   // [rows][slices]: m, z, index of m
-  uint64_t* best; // [B][2]: the residual's race, p's own
+  float4* part;   // [B][K + 1][pieces]: m, z, best score (relative to m), its index (greedy: of m)
+  uint64_t* best; // [B]: the residual's race
   uint32_t* done; // [B]: workgroups that have raced
-  int32_t B, K, V, slices, slice, races, race;
+  int32_t B, K, V, pieces, groups, races, race;
 };
 
 // Sequence b's factor of the exponent (log2 e / T) and whether it is greedy.  The factor stays finite and above 0, so
@@ -46,9 +54,27 @@ __device__ inline int drafted(const VerifyArgs& a, int b) {
   return a.draft_len ? min(max(a.draft_len[b], 0), a.K) : a.K;
 }
 
+// 8 entries as they are in memory, in whole registers.
 template <typename T>
 struct Raw {
-  T x[8];
+  static constexpr int N = sizeof(T) * 2;
+  uint32_t w[N];
+  __device__ float at(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    if constexpr (std::is_same<T, bf16_t>::value) return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+    return (float)__builtin_bit_cast(f16_t, (uint16_t)(w[i / 2] >> (i & 1) * 16));
+  }
+  // the first 8 entries, of which `have` exist (the others read as the last)
+  __device__ void load_short(const T* row, int have) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      constexpr int E = 4 / sizeof(T);
+      T e[E];
+#pragma unroll
+      for (int k = 0; k < E; ++k) e[k] = row[min(i * E + k, have - 1)];
+      __builtin_memcpy(&w[i], e, 4);
+    }
+  }
 };
 
 // Rows of odd vocabularies start anywhere: 16-byte loads from any address that fits the type.
@@ -57,7 +83,7 @@ __device__ inline void load8(const T* p, float (&x)[8]) {
   Raw<T> r;
   __builtin_memcpy(&r, p, sizeof(r));
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = (float)r.x[i];
+  for (int i = 0; i < 8; ++i) x[i] = r.at(i);
 }
 
 // 8 entries from token t on; those at or after V read as `other`.
@@ -74,75 +100,200 @@ __device__ inline uint32_t bits8(const uint32_t* mask, int t, int V) {
   return m;
 }
 
-struct Online {
-  float m, z;
+// Across a wave, by lanes' exchanges that need no LDS: f of all lanes in every lane.
+template <typename F>
+__device__ inline uint32_t across(uint32_t x, F f) {
+  x = f(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xF, 0xF, true));   // lane ^ 1
+  x = f(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true));   // lane ^ 2
+  x = f(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x141, 0xF, 0xF, true));  // 7 - lane, of 8
+  x = f(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x140, 0xF, 0xF, true));  // 15 - lane, of 16
+  auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = f(r[0], r[1]);
+  r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return f(r[0], r[1]);
+}
+__device__ inline float max_across(float x) {
+  return __uint_as_float(across(__float_as_uint(x), [](uint32_t p, uint32_t q) {
+    return __float_as_uint(fmaxf(__uint_as_float(p), __uint_as_float(q)));
+  }));
+}
+__device__ inline float sum_across(float x) {
+  return __uint_as_float(across(__float_as_uint(x), [](uint32_t p, uint32_t q) {
+    return __float_as_uint(__uint_as_float(p) + __uint_as_float(q));
+  }));
+}
+__device__ inline int min_across(int x) {
+  return (int)across((uint32_t)x, [](uint32_t p, uint32_t q) { return (uint32_t)min((int)p, (int)q); });
+}
+
+// What is known of some of a row's tokens.  score: the largest w / noise, relative to m as w is; idx: its lowest index,
+// or of a greedy row the lowest index of m.
+struct Row {
+  float m, z, score;
   int idx;
-  __device__ static Online empty() { return {kLow, 0.f, 0x7FFFFFFF}; }
-  __device__ void take(const float (&x)[8], uint32_t bits, int t, float c, bool greedy) {
-    float v[8], top = kLow;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      v[i] = bits >> i & 1 ? x[i] : -INFINITY;
-      top = fmaxf(top, v[i]);
-    }
-    if (top > m || (idx == 0x7FFFFFFF && greedy)) {
-      if (greedy) {
-#pragma unroll
-        for (int i = 7; i >= 0; --i)
-          if (v[i] == top) idx = t + i;
-      }
-      z *= __builtin_amdgcn_exp2f((m - top) * c);
-      m = top;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) z += __builtin_amdgcn_exp2f((v[i] - m) * c);
-  }
-  __device__ void join(float om, float oz, int oi, float c) {
-    const float top = fmaxf(m, om);
-    z = z * __builtin_amdgcn_exp2f((m - top) * c) + oz * __builtin_amdgcn_exp2f((om - top) * c);
-    idx = om > m ? oi : om == m ? min(idx, oi) : idx;
-    m = top;
-  }
-  __device__ void across(float c) {
-    for (int o = 32; o > 0; o >>= 1) {
-      const float om = __shfl_xor(m, o), oz = __shfl_xor(z, o);
-      const int oi = __shfl_xor(idx, o);
-      join(om, oz, oi, c);
-    }
-  }
 };
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void stats_kernel(VerifyArgs a) {
-  const int tid = (int)threadIdx.x, slice = (int)blockIdx.x % a.slices, r = (int)blockIdx.x / a.slices;
-  const int b = r / (a.K + 1), j = r - b * (a.K + 1);
-  if (j == 0 && slice == 0 && tid == 0) {
-    a.best[2 * b] = a.best[2 * b + 1] = 0;
+// The lanes' parts of a row as one, in every lane.
+__device__ inline Row join_lanes(Row r, float c, bool greedy) {
+  const float m = max_across(r.m), f = __builtin_amdgcn_exp2f((r.m - m) * c);
+  const float s = r.score * f, best = max_across(s);
+  const int idx = min_across((greedy ? r.m == m : s == best) ? r.idx : kNone);
+  return {m, sum_across(r.z * f), best, idx};
+}
+
+// A workgroup takes a piece of the rows of one sequence that are in one group.
+enum class Rows { kAll, kMasked, kShort };  // all tokens allowed, mask rows, fewer than 8 tokens (masked or not)
+
+template <typename T, bool GREEDY, Rows ROWS>
+__device__ __forceinline__ void scan(const VerifyArgs& a, Row (&wave_row)[2][kWaves], int b, int piece, int from, int to,
+                                     int n, float c) {
+  constexpr int S = kSteps<T>;
+  const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const T* rows = (const T*)a.logits + b * a.ls[0];
+  const uint32_t* masks = a.mask ? a.mask + b * a.ms[0] : nullptr;
+  // (scalar loads, which do not wait for those of the rows)
+  const auto* drafts = (const __attribute__((address_space(4))) int32_t*)(a.draft + (int64_t)b * a.K);
+  const int t0 = (piece * kWaves + wave) * S * 512 + lane * 8;
+  // A step's 8 tokens start at a multiple of 8, t0 + 512 s.  At the end of a row the 8 last ones are read instead, with
+  // the bits of those before t0 + 512 s cleared; a vocabulary of less than 8 has one such step only.
+  const auto base = [&](int s) { return max(min(t0 + s * 512, a.V - 8), 0); };
+
+  float rate[S][8];  // 1 / noise
+  if constexpr (!GREEDY) {
+    const float* e = a.noise + b * a.ns;
+    if constexpr (ROWS != Rows::kShort) {
+#pragma unroll
+      for (int s = 0; s < S; ++s) load8(e + base(s), rate[s]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) rate[0][i] = e[min(i, a.V - 1)];
+    }
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) rate[s][i] = __builtin_amdgcn_rcpf(rate[s][i]);
+  }
+
+  // The mask two rows ahead, the logits one, without branches: what is on its way stays countable.  Where none of its 8
+  // tokens is allowed a lane reads the row's first ones, as all such lanes do.
+  uint32_t bits[2][S];
+  Raw<T> raw[2][S];
+  const auto get_bits = [&](int j, uint32_t (&x)[S]) {
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      const int t = t0 + s * 512, last = min(t, a.V - 1);
+      uint32_t m = 0xFFu;
+      if (ROWS == Rows::kMasked || (ROWS == Rows::kShort && masks)) m = ((const uint8_t*)(masks + j * a.ms[1]))[last >> 3];
+      m &= (1u << min(max(a.V - t, 0), 8)) - 1u;
+      x[s] = m << (t - base(s) & 7);
+    }
+  };
+  const auto get_logits = [&](int j, const uint32_t (&x)[S], Raw<T> (&y)[S]) {
+    const T* row = rows + j * a.ls[1];
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      if constexpr (ROWS != Rows::kShort)
+        __builtin_memcpy(y[s].w, row + (x[s] ? base(s) : 0), sizeof(y[s].w));
+      else if (s == 0)
+        y[s].load_short(row, a.V);
+    }
+  };
+  const auto judge = [&](int j, const uint32_t (&x)[S], const Raw<T> (&y)[S]) {
+    Row r = {kLow, 0.f, 0.f, kNone};
+    // a lane's tokens by number, s * 8 + i: the best one's, and that of a certain draft, which takes no part in its row's race
+    int code = -1, leave = -1;
+    if (!GREEDY && !a.probs && j < n) {
+      const int d = drafts[j], s = (d - t0) >> 9;
+      if (d >= t0 && s < S && d - t0 - s * 512 < 8 && d < a.V) leave = s * 8 + d - base(s);
+    }
+    const bool here = __any(leave >= 0);
+    uint32_t any = 0;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      any |= x[s];
+      if (!__any(x[s] != 0)) continue;
+      float v[8], top = r.m;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[i] = x[s] >> i & 1 ? y[s].at(i) : -INFINITY;
+        top = fmaxf(top, v[i]);
+      }
+      if constexpr (GREEDY)
+        if (top > r.m || code < 0)
+#pragma unroll
+          for (int i = 7; i >= 0; --i) code = v[i] == top ? s * 8 + i : code;
+      const float f = __builtin_amdgcn_exp2f((r.m - top) * c);
+      r.m = top;
+      r.z *= f;
+      r.score *= f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float w = __builtin_amdgcn_exp2f((v[i] - top) * c);
+        r.z += w;
+        if constexpr (!GREEDY) v[i] = w * rate[s][i];
+      }
+      if constexpr (!GREEDY) {
+        if (here)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) v[i] = s * 8 + i == leave ? 0.f : v[i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          code = v[i] > r.score ? s * 8 + i : code;
+          r.score = fmaxf(r.score, v[i]);
+        }
+      }
+    }
+    r.idx = code < 0 ? kNone : base(code / 8) + code % 8;
+    if (__any(any != 0)) r = join_lanes(r, c, GREEDY);
+    // the waves' parts meet; two rows' slots in turn, so one barrier a row is enough
+    if (lane == 0) wave_row[j & 1][wave] = r;
+    __syncthreads();
+    if (wave == 0) {
+      r = lane < kWaves ? wave_row[j & 1][lane] : Row{kLow, 0.f, 0.f, kNone};
+      r = join_lanes(r, c, GREEDY);
+      if (lane == 0)
+        a.part[((int64_t)b * (a.K + 1) + j) * a.pieces + piece] = make_float4(r.m, r.z, r.score, __int_as_float(r.idx));
+    }
+  };
+
+  get_bits(from, bits[0]);
+  get_logits(from, bits[0], raw[0]);
+  if (from + 1 < to) get_bits(from + 1, bits[1]);
+  for (int j = from; j < to; j += 2) {
+    // rows j and j + 1, whose buffers are 0 and 1
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      if (j + k >= to) break;
+      uint32_t now[S];
+#pragma unroll
+      for (int s = 0; s < S; ++s) now[s] = bits[k][s];
+      if (j + k + 1 < to) get_logits(j + k + 1, bits[k ^ 1], raw[k ^ 1]);
+      if (j + k + 2 < to) get_bits(j + k + 2, bits[k]);
+      judge(j + k, now, raw[k]);
+    }
+  }
+}
+
+template <typename T, Rows ROWS>
+__global__ __launch_bounds__(kThreads, 3) void scan_kernel(VerifyArgs a) {
+  // The groups of one piece of a sequence are 8 workgroups apart: on one die, whose cache then holds their noise.
+  const uint32_t units = (uint32_t)a.B * (uint32_t)a.pieces, eight = blockIdx.x / (8u * (uint32_t)a.groups);
+  const uint32_t in = blockIdx.x - eight * 8u * (uint32_t)a.groups, unit = eight * 8 + in % 8;
+  if (unit >= units) return;
+  const int group = (int)(in / 8), piece = (int)(unit % (uint32_t)a.pieces), b = (int)(unit / (uint32_t)a.pieces);
+  if (piece == 0 && group == 0 && threadIdx.x == 0) {
+    a.best[b] = 0;
     a.done[b] = 0;
   }
-  if (j > drafted(a, b)) return;
+  const int n = drafted(a, b), from = group * (a.K + 1) / a.groups, to = min((group + 1) * (a.K + 1) / a.groups, n + 1);
+  if (from >= to) return;
+  __shared__ Row wave_row[2][kWaves];
   bool greedy;
   const float c = factor_of(a, b, greedy);
-  const T* row = (const T*)a.logits + b * a.ls[0] + j * a.ls[1];
-  const uint32_t* mask = a.mask ? a.mask + b * a.ms[0] + j * a.ms[1] : nullptr;
-  const int end = min(a.V, (slice + 1) * a.slice);
-  Online o = Online::empty();
-  for (int t = slice * a.slice + tid * 8; t < end; t += kStep) {
-    float x[8];
-    if (t + 8 <= a.V)
-      load8(row + t, x);
-    else
-      load8_end(row, t, a.V, -INFINITY, x);
-    o.take(x, bits8(mask, t, a.V), t, c, greedy);
-  }
-  o.across(c);
-  __shared__ Online wave[kThreads / 64];
-  if ((tid & 63) == 0) wave[tid >> 6] = o;
-  __syncthreads();
-  if (tid == 0) {
-    for (int w = 1; w < kThreads / 64; ++w) o.join(wave[w].m, wave[w].z, wave[w].idx, c);
-    a.part[(int64_t)r * a.slices + slice] = make_float4(o.m, o.z, __int_as_float(o.idx), 0.f);
-  }
+  if (greedy)
+    scan<T, true, ROWS>(a, wave_row, b, piece, from, to, n, c);
+  else
+    scan<T, false, ROWS>(a, wave_row, b, piece, from, to, n, c);
 }
 
 __device__ inline uint64_t race_key(float score, int t) {
@@ -166,109 +317,99 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(VerifyArgs a) {
   const int n = drafted(a, b);
   const T* rows = (const T*)a.logits + b * a.ls[0];
   const uint32_t* masks = a.mask ? a.mask + b * a.ms[0] : nullptr;
-  __shared__ Online row[64];
+  __shared__ Row row[64];
   __shared__ int first;
-  __shared__ uint64_t wave_best[2][kThreads / 64];
-  for (int j = tid >> 6; j <= n; j += kThreads / 64) {
-    Online o = Online::empty();
-    if (lane < a.slices) {
-      const float4 p = a.part[((int64_t)b * (a.K + 1) + j) * a.slices + lane];
-      o.m = p.x;
-      o.z = p.y;
-      o.idx = __float_as_int(p.z);
+  // the lane's draft, and what is known of it without its row's sums
+  int x = -1;
+  bool allowed = false;
+  float l = 0.f, uq = 0.f;
+  if (tid < n) {
+    x = a.draft[(int64_t)b * a.K + tid];
+    if ((uint32_t)x < (uint32_t)a.V) {
+      l = (float)rows[tid * a.ls[1] + x];
+      allowed = !masks || (masks[tid * a.ms[1] + (x >> 5)] >> (x & 31) & 1);
+      if (!greedy) uq = a.uniform[(int64_t)b * a.K + tid] * (a.probs ? a.probs[b * a.ps[0] + tid * a.ps[1] + x] : 1.f);
     }
-    o.across(c);
-    if (lane == 0) row[j] = o;
+  }
+  for (int j = tid >> 6; j <= n; j += kThreads / 64) {
+    Row r = {kLow, 0.f, 0.f, kNone};
+    for (int p = lane; p < a.pieces; p += 64) {
+      const float4 y = a.part[((int64_t)b * (a.K + 1) + j) * a.pieces + p];
+      const float m = fmaxf(r.m, y.x), f = __builtin_amdgcn_exp2f((r.m - m) * c), g = __builtin_amdgcn_exp2f((y.x - m) * c);
+      const int idx = __float_as_int(y.w);
+      if (greedy ? y.x > r.m || r.idx == kNone : y.z * g > r.score * f) r.idx = idx;  // pieces in order: the lowest
+      r.score = fmaxf(r.score * f, y.z * g);
+      r.z = r.z * f + y.y * g;
+      r.m = m;
+    }
+    r = join_lanes(r, c, greedy);
+    if (lane == 0) row[j] = r;
   }
   __syncthreads();
-  // weight of token t in row j, 0 where it is not allowed
-  auto weight = [&](int j, int t) {
-    if ((uint32_t)t >= (uint32_t)a.V || (masks && !(masks[j * a.ms[1] + (t >> 5)] >> (t & 31) & 1))) return 0.f;
-    return __builtin_amdgcn_exp2f(((float)rows[j * a.ls[1] + t] - row[j].m) * c);
-  };
   if (tid < 64) {
     bool ok = false;
-    if (tid < n) {
-      const int x = a.draft[(int64_t)b * a.K + tid];
-      const float z = row[tid].z;
-      if (z > 0.f && (uint32_t)x < (uint32_t)a.V) {
-        if (greedy) {
-          ok = x == row[tid].idx;
-        } else {
-          const float q = a.probs ? a.probs[b * a.ps[0] + tid * a.ps[1] + x] : 1.f;
-          ok = a.uniform[(int64_t)b * a.K + tid] * q < weight(tid, x) / z;
-        }
-      }
-    }
+    if (tid < n && allowed && row[tid].z > 0.f)
+      ok = greedy ? x == row[tid].idx : uq < __builtin_amdgcn_exp2f((l - row[tid].m) * c) / row[tid].z;
     const uint64_t refused = __ballot(!ok);  // lane n refuses (n <= 63)
     if (tid == 0) first = __builtin_ctzll(refused);
   }
   __syncthreads();
   const int at = first;
-  const Online o = row[at];
-  const bool alive = o.z > 0.f;  // not for NaN
-  int token = -1;
-  if (greedy) {
-    if (alive) token = o.idx;
-  } else {
-    // the race over this workgroup's part of row `at`
-    const int x = at < n ? a.draft[(int64_t)b * a.K + at] : -1;
-    const float* q = at < n && a.probs ? a.probs + b * a.ps[0] + at * a.ps[1] : nullptr;
-    const T* lrow = rows + at * a.ls[1];
-    const uint32_t* mask = masks ? masks + at * a.ms[1] : nullptr;
-    const float* noise = a.noise + b * a.ns;
-    const float over = 1.f / o.z;
-    uint64_t left = 0, whole = 0;
-    const int end = alive ? min(a.V, (part + 1) * a.race) : 0;
-    for (int t = part * a.race + tid * 8; t < end; t += kStep) {
-      float l[8], e[8], d[8];
-      if (t + 8 <= a.V) {
-        load8(lrow + t, l);
-        load8(noise + t, e);
-        if (q) load8(q + t, d);
-      } else {
-        load8_end(lrow, t, a.V, -INFINITY, l);
-        load8_end(noise, t, a.V, 1.f, e);
-        if (q) load8_end(q, t, a.V, 0.f, d);
-      }
-      const uint32_t bits = bits8(mask, t, a.V);
+  const Row o = row[at];
+  int token = o.z > 0.f && o.idx != kNone ? o.idx : -1;  // o.z is not above 0 where it is NaN
+  if (!greedy && o.z > 0.f && at < n) {
+    const int refused = a.draft[(int64_t)b * a.K + at];
+    if (!a.probs) {
+      if (token < 0) token = refused;  // the draft was all that is allowed
+    } else {
+      // the race over this workgroup's part of what is left of row `at`
+      const float* q = a.probs + b * a.ps[0] + at * a.ps[1];
+      const T* lrow = rows + at * a.ls[1];
+      const uint32_t* mask = masks ? masks + at * a.ms[1] : nullptr;
+      const float* noise = a.noise + b * a.ns;
+      const float over = 1.f / o.z;
+      uint64_t left = 0;
+      const int end = min(a.V, (part + 1) * a.race);
+      for (int t = part * a.race + tid * 8; t < end; t += kStep) {
+        const uint32_t bits = bits8(mask, t, a.V);
+        if (!bits) continue;
+        float y[8], e[8], d[8];
+        if (t + 8 <= a.V) {
+          load8(lrow + t, y);
+          load8(noise + t, e);
+          load8(q + t, d);
+        } else {
+          load8_end(lrow, t, a.V, -INFINITY, y);
+          load8_end(noise, t, a.V, 1.f, e);
+          load8_end(q, t, a.V, 0.f, d);
+        }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float p = bits >> i & 1 ? __builtin_amdgcn_exp2f((l[i] - o.m) * c) * over : 0.f;
-        const float rate = __builtin_amdgcn_rcpf(e[i]);
-        const float rest = q ? fmaxf(p - d[i], 0.f) : t + i == x ? 0.f : p;
-        left = max(left, race_key(rest * rate, t + i));
-        whole = max(whole, race_key(p * rate, t + i));
+        for (int i = 0; i < 8; ++i) {
+          const float p = bits >> i & 1 ? __builtin_amdgcn_exp2f((y[i] - o.m) * c) * over : 0.f;
+          left = max(left, race_key(fmaxf(p - d[i], 0.f) * __builtin_amdgcn_rcpf(e[i]), t + i));
+        }
       }
-    }
-    left = max_across(left);
-    whole = max_across(whole);
-    if (lane == 0) {
-      wave_best[0][tid >> 6] = left;
-      wave_best[1][tid >> 6] = whole;
-    }
-    __syncthreads();
-    __shared__ bool last;
-    if (tid == 0) {
-      for (int w = 1; w < kThreads / 64; ++w) {
-        left = max(left, wave_best[0][w]);
-        whole = max(whole, wave_best[1][w]);
+      left = max_across(left);
+      __shared__ uint64_t wave_best[kThreads / 64];
+      __shared__ bool last;
+      if (lane == 0) wave_best[tid >> 6] = left;
+      __syncthreads();
+      if (tid == 0) {
+        for (int w = 1; w < kThreads / 64; ++w) left = max(left, wave_best[w]);
+        unsigned long long* best = (unsigned long long*)a.best + b;
+        // Both are atomics at the device's point of coherence, and the first is done before the second begins: no fence
+        // over other memory is needed, for nothing else passes between the workgroups.
+        __hip_atomic_fetch_max(best, left, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        last = __hip_atomic_fetch_add(a.done + b, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)a.races - 1;
+        if (last) wave_best[0] = __hip_atomic_fetch_max(best, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
-      unsigned long long* best = (unsigned long long*)(a.best + 2 * b);
-      __hip_atomic_fetch_max(best, left, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      __hip_atomic_fetch_max(best + 1, whole, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      last = __hip_atomic_fetch_add(a.done + b, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)a.races - 1;
-      if (last) {
-        left = __hip_atomic_load(best, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        whole = __hip_atomic_load(best + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        wave_best[0][0] = left ? left : whole;
-      }
+      __syncthreads();
+      if (!last) return;
+      if (const uint64_t key = wave_best[0]) token = (int)~(uint32_t)key;  // otherwise p itself
     }
-    __syncthreads();
-    if (!last) return;
-    const uint64_t key = wave_best[0][0];
-    if (key) token = (int)~(uint32_t)key;
   }
+  if (part > 0 && !(a.probs && !greedy && o.z > 0.f && at < n)) return;
   if (tid <= a.K) {
     const int mine = tid < at ? a.draft[(int64_t)b * a.K + tid] : tid == at ? token : -1;
     float lp = 0.f;
@@ -279,29 +420,30 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(VerifyArgs a) {
   if (tid == 0) a.accepted[b] = at;
 }
 
-// How many pieces `units` rows of V tokens are cut into, and their tokens: about 2048 workgroups in all, none of less
-// than two steps, so that short batches fill the chip and long ones are not cut at all.
-void pieces(int64_t units, int V, int most, int32_t& n, int32_t& len) {
-  const int64_t want = std::max<int64_t>(1, (2048 + units - 1) / units);
-  const int fit = std::max(1, (V + 2 * kStep - 1) / (2 * kStep));
-  n = (int32_t)std::min<int64_t>({want, fit, most});
-  len = (int32_t)((((int64_t)V + n - 1) / n + kStep - 1) / kStep * kStep);
-  n = (int32_t)(((int64_t)V + len - 1) / len);
+// The launch.  A workgroup goes over rows of a sequence with its piece of the noise; the rows are dealt to so many groups
+// that there are about 4096 workgroups.  The residual's race is cut into about 1024 workgroups, none of less than a step.
+void plan(VerifyArgs& a, int steps) {
+  a.pieces = (int32_t)(((int64_t)a.V + steps * kPiece - 1) / (steps * kPiece));
+  const int64_t all = (int64_t)a.B * a.pieces;
+  a.groups = (int32_t)std::min<int64_t>(a.K + 1, (4096 + all - 1) / all);
+  const int64_t want = std::max<int64_t>(1, 1024 / a.B), fit = ((int64_t)a.V + kStep - 1) / kStep;
+  const int64_t n = std::min(want, fit);
+  a.race = (int32_t)((((int64_t)a.V + n - 1) / n + kStep - 1) / kStep * kStep);
+  a.races = (int32_t)(((int64_t)a.V + a.race - 1) / a.race);
 }
 
 bool sizes_ok(int32_t B, int32_t K, int32_t V) {
   return B >= 1 && B <= 65535 && K >= 0 && K <= 63 && V >= 1 && V <= INT32_MAX - 2 * kStep;
 }
 
-size_t head_bytes(int32_t B) { return ((size_t)B * 20 + 255) / 256 * 256; }
+size_t head_bytes(int32_t B) { return ((size_t)B * 12 + 255) / 256 * 256; }
 
 }  // namespace
 
 extern "C" size_t grid_verify_workspace_bytes(int32_t B, int32_t K, int32_t V) {
   if (!sizes_ok(B, K, V)) return 0;
-  int32_t n, len;
-  pieces((int64_t)B * (K + 1), V, kMaxSlices, n, len);
-  return head_bytes(B) + (size_t)B * (size_t)(K + 1) * (size_t)n * sizeof(float4);
+  const size_t pieces = ((size_t)V + kSteps<float> * kPiece - 1) / (kSteps<float> * kPiece);  // 16-bit rows have fewer
+  return head_bytes(B) + (size_t)B * (size_t)(K + 1) * pieces * sizeof(float4);
 }
 
 extern "C" int grid_verify(const grid_verify_args* args, void* stream) {
@@ -339,21 +481,26 @@ extern "C" int grid_verify(const grid_verify_args* args, void* stream) {
   a.accepted = g.accepted;
   a.logprobs = g.logprobs;
   a.best = (uint64_t*)g.workspace;
-  a.done = (uint32_t*)(a.best + 2 * (size_t)g.B);
+  a.done = (uint32_t*)(a.best + (size_t)g.B);
   a.part = (float4*)((uint8_t*)g.workspace + head_bytes(g.B));
   a.B = g.B;
   a.K = g.K;
   a.V = g.V;
-  const int64_t rows = (int64_t)g.B * (g.K + 1);
-  pieces(rows, g.V, kMaxSlices, a.slices, a.slice);
-  pieces(g.B, g.V, 1 << 20, a.races, a.race);
-  if (!g.noise) a.races = 1;
+  plan(a, g.dtype == GRID_DTYPE_F32 ? kSteps<float> : kSteps<bf16_t>);
+  if (!g.noise || !g.draft_probs) a.races = 1;
+  const int64_t one = ((int64_t)g.B * a.pieces + 7) / 8 * 8 * a.groups, two = (int64_t)g.B * a.races;
+  if (one > 1 << 23 || two > 1 << 23) return fail(GRID_E_CAPACITY, "grid_verify: too many rows for one launch");
   hipStream_t s = (hipStream_t)stream;
-  const dim3 one((unsigned)(rows * a.slices)), two((unsigned)((int64_t)g.B * a.races));
   auto launch = [&](auto type) {
     using T = decltype(type);
-    hipLaunchKernelGGL(stats_kernel<T>, one, dim3(kThreads), 0, s, a);
-    hipLaunchKernelGGL(pick_kernel<T>, two, dim3(kThreads), 0, s, a);
+    const dim3 blocks((unsigned)one), threads(kThreads);
+    if (g.V < 8)
+      hipLaunchKernelGGL((scan_kernel<T, Rows::kShort>), blocks, threads, 0, s, a);
+    else if (g.mask)
+      hipLaunchKernelGGL((scan_kernel<T, Rows::kMasked>), blocks, threads, 0, s, a);
+    else
+      hipLaunchKernelGGL((scan_kernel<T, Rows::kAll>), blocks, threads, 0, s, a);
+    hipLaunchKernelGGL(pick_kernel<T>, dim3((unsigned)two), dim3(kThreads), 0, s, a);
   };
   if (g.dtype == GRID_DTYPE_F32)
     launch(float());
