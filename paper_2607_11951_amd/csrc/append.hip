@@ -1,8 +1,9 @@
 // append.hip -- grid_kv_append: keys, values and queries of new tokens into a paged cache (gfx950).
 //
 // A head's vector of one token is 8 entries (16 bytes) a lane, so a power of two of lanes holds one; its mean square is
-// a butterfly over those lanes.  Both entries of a rotated pair are needed at once: side by side they are in one lane;
+// their sum across those lanes.  Both entries of a rotated pair are needed at once: side by side they are in one lane;
 // half a rotation apart the partner's 16 bytes are exchanged between the lanes.
+#include "lanes.h"
 #include "paged.h"
 
 using namespace grid;
@@ -18,7 +19,7 @@ struct AppendArgs {
   const float *cos, *sin, *q_norm, *k_norm;
   int32_t* status;
   int32_t hq, n_positions, half, interleaved;  // half = rot_dim / 2
-  float eps;
+  float eps, over;  // over = 1 / head_dim
   int32_t lanes;  // lanes of a head's vector
 };
 
@@ -38,48 +39,13 @@ __device__ int status_of(const Paged& P, const AppendArgs& a, int b) {
   return ok ? GRID_ROW_OK : GRID_ROW_BAD_CONFIG;
 }
 
-template <typename T>
-__device__ void turn(float (&x)[8], const AppendArgs& a, const float* weight, int D, int part, int pos) {
-  const int e = part * 8;  // the lane's first entry
-  if (weight) {
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s += x[i] * x[i];
-    if (e >= D) s = 0.f;
-    for (int o = a.lanes >> 1; o > 0; o >>= 1) s += __shfl_xor(s, o);
-    const float r = 1.0f / sqrtf(s / (float)D + a.eps);
-    if (e < D)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] *= r * weight[e + i];
-  }
-  if (!a.cos) return;
-  const float* cs = a.cos + (int64_t)pos * a.half;
-  const float* sn = a.sin + (int64_t)pos * a.half;
-  if (a.interleaved) {
-    if (e < 2 * a.half)
-#pragma unroll
-      for (int i = 0; i < 8; i += 2) {
-        const float c = cs[(e + i) / 2], s = sn[(e + i) / 2], u = x[i], v = x[i + 1];
-        x[i] = u * c - v * s;
-        x[i + 1] = v * c + u * s;
-      }
-    return;
-  }
-  const int hp = a.half / 8;  // the partner's distance in lanes
-  const bool low = part < hp, in = part < 2 * hp;
-  const int lane = (int)threadIdx.x & 63, from = in ? (low ? lane + hp : lane - hp) : lane;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float y = __shfl(x[i], from);
-    if (in) {
-      const int j = (low ? e : e - a.half) + i;
-      x[i] = low ? x[i] * cs[j] - y * sn[j] : x[i] * cs[j] + y * sn[j];
-    }
-  }
-}
+enum class Turn { kNone, kHalves, kPairs };
 
-// One workgroup a token; the workgroups after the last token write the statuses.
-template <typename T>
+// One workgroup a token; the workgroups after the last token write the statuses.  What a token needs hangs on reads one
+// after the other (its sequence and lengths, its page, its cosines), so the vectors, which hang on nothing, are asked for
+// first, and the sequence's lengths with its search: the lanes hold those of 64 sequences, and the one that is found hands
+// its own out.  A lane takes the same entries of all its vectors: the cosines are read once.
+template <typename T, Turn TURN, bool NORM>
 __global__ __launch_bounds__(kThreads) void append_kernel(Paged P, AppendArgs a) {
   const int t = (int)blockIdx.x, tid = (int)threadIdx.x, lane = tid & 63;
   if (t >= P.T) {
@@ -87,47 +53,132 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Paged P, AppendArgs a)
     if (b < P.B) a.status[b] = status_of(P, a, b);
     return;
   }
+  const int part = tid & (a.lanes - 1), groups = kThreads / a.lanes, e = part * 8;  // e: the lane's first entry
+  const int u_first = e < P.D ? tid / a.lanes : 1 << 30, vectors = 2 * P.hkv + a.hq;
+  constexpr int AHEAD = 3;  // vectors that a lane asks for before it knows where they go
+  const auto source = [&](int u) {
+    const int h = u < P.hkv ? u : u < 2 * P.hkv ? u - P.hkv : u - 2 * P.hkv;
+    const uint16_t* src = u < P.hkv ? a.kin + t * a.ks[0] + h * a.ks[1]
+                          : u < 2 * P.hkv ? a.vin + t * a.vs[0] + h * a.vs[1] : a.qin + t * a.qs[0] + h * a.qs[1];
+    return *(const Eight<T>*)(src + e);
+  };
+  __shared__ __attribute__((aligned(16))) float weights[2][256];  // of keys, of queries
+  if constexpr (NORM)
+    for (int i = tid; i < P.D; i += kThreads) {
+      if (a.k_norm) weights[0][i] = a.k_norm[i];
+      if (a.q_norm) weights[1][i] = a.q_norm[i];
+    }
+  Eight<T> ahead[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (u_first + i * groups < vectors) ahead[i] = source(u_first + i * groups);
   // the token's sequence: as many as end at or before it
+  Chunk c;
+  c.ok = false;
   int b = 0;
-  for (int s = 0; s < P.B; s += 64)
-    b += __popcll(__ballot(s + lane < P.B && P.cu_q[s + lane + 1] <= t));
-  if (b >= P.B) return;
-  const Chunk c = chunk_of(P, b);
+  for (int s = 0; s < P.B; s += 64) {
+    const int x = min(s + lane, P.B - 1);
+    const int32_t first = P.cu_q[x], end = P.cu_q[x + 1], kv = P.kv_len[x];
+    const int before = __popcll(__ballot(s + lane < P.B && end <= t));
+    b += before;
+    if (before < min(64, P.B - s)) {
+      c = chunk_of(P, __builtin_amdgcn_readlane(first, before), __builtin_amdgcn_readlane(end, before),
+                   __builtin_amdgcn_readlane(kv, before));
+      break;
+    }
+  }
   if (!c.ok || t < c.first || t >= c.first + c.n) return;
   const int pos = c.kv - c.n + t - c.first;
-  if (a.cos && pos >= a.n_positions) return;
+  if (TURN != Turn::kNone && pos >= a.n_positions) return;
   uint32_t row;
   const int page = P.page_of(b, (uint32_t)pos, row);
+  // the rotation of the lane's entries; in halves, hp lanes apart: the partner's lane and entries
+  float cs[8], sn[8];
+  const int hp = a.half / 8;
+  const bool low = part < hp, turned = e < 2 * a.half;
+  const int other = low ? lane + hp : lane - hp, oe = low ? e + a.half : e - a.half;
+  if (TURN != Turn::kNone && turned) {
+    constexpr int N = TURN == Turn::kPairs ? 4 : 8;
+    const int64_t at = (int64_t)pos * a.half + (TURN == Turn::kPairs ? e / 2 : low ? e : oe);
+    __builtin_memcpy(cs, a.cos + at, N * 4);
+    __builtin_memcpy(sn, a.sin + at, N * 4);
+  }
   if (!P.in_cache(page)) return;
-  const int part = tid & (a.lanes - 1), group = tid / a.lanes, groups = kThreads / a.lanes;
-  const bool real = part * 8 < P.D;
-  const int vectors = 2 * P.hkv + a.hq;
-  // every lane of a wave takes the same number of steps: the exchanges need them all
-  for (int u0 = 0; u0 < vectors; u0 += groups) {
-    const int u = u0 + group;
-    const bool mine = real && u < vectors;
-    const int kind = u < P.hkv ? 0 : u < 2 * P.hkv ? 1 : 2;
-    const int h = kind == 0 ? u : kind == 1 ? u - P.hkv : u - 2 * P.hkv;
-    Eight<T> in = {};
-    if (mine) {
-      const uint16_t* src = kind == 0 ? a.kin + t * a.ks[0] + h * a.ks[1]
-                            : kind == 1 ? a.vin + t * a.vs[0] + h * a.vs[1] : a.qin + t * a.qs[0] + h * a.qs[1];
-      in = *(const Eight<T>*)(src + part * 8);
-    }
-    const float* weight = kind == 2 ? a.q_norm : a.k_norm;
-    float x[8];
+  if constexpr (NORM) __syncthreads();
+  const auto store = [&](int u, Eight<T> in) {
+    const bool key = u < P.hkv, value = !key && u < 2 * P.hkv, normed = NORM && (key ? a.k_norm : a.q_norm);
+    const float* weight = weights[key ? 0 : 1];
+    float x[8], r = 1.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = (float)in.x[i];
-    turn<T>(x, a, weight, P.D, part, pos);
-    if (!mine) continue;
-    uint16_t* dst = kind == 0 ? P.k + page * P.ks[0] + row * P.ks[1] + h * P.ks[2]
-                    : kind == 1 ? P.v + page * P.vs[0] + row * P.vs[1] + h * P.vs[2] : a.qout + t * a.os[0] + h * a.os[1];
-    Eight<T> out = in;
-    if (kind != 1 && (weight || a.cos))
+    if constexpr (NORM) {
+      float s = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) out.x[i] = (T)x[i];
-    *(Eight<T>*)(dst + part * 8) = out;
+      for (int i = 0; i < 8; ++i) s += x[i] * x[i];
+      if (e >= P.D) s = 0.f;
+      s = sum_across(s, a.lanes);
+      if (normed) {
+        r = __builtin_amdgcn_rsqf(s * a.over + a.eps);
+        if (e < P.D)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] *= r * weight[e + i];
+      }
+    }
+    if constexpr (TURN == Turn::kPairs) {
+      if (turned)
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+          const float p = x[i], q = x[i + 1];
+          x[i] = p * cs[i / 2] - q * sn[i / 2];
+          x[i + 1] = q * cs[i / 2] + p * sn[i / 2];
+        }
+    }
+    if constexpr (TURN == Turn::kHalves) {
+      // the partner's entries as they came, normed here
+      uint32_t w[4];
+      __builtin_memcpy(w, &in, 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = (uint32_t)__shfl((int)w[i], turned ? other : lane);
+      Eight<T> y;
+      __builtin_memcpy(&y, w, 16);
+      if (turned)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float z = (float)y.x[i];
+          if (normed) z *= r * weight[oe + i];
+          x[i] = low ? x[i] * cs[i] - z * sn[i] : x[i] * cs[i] + z * sn[i];
+        }
+    }
+    if (u >= vectors) return;
+    const int h = key ? u : value ? u - P.hkv : u - 2 * P.hkv;
+    uint16_t* dst = key ? P.k + page * P.ks[0] + row * P.ks[1] + h * P.ks[2]
+                    : value ? P.v + page * P.vs[0] + row * P.vs[1] + h * P.vs[2] : a.qout + t * a.os[0] + h * a.os[1];
+    if (!value && (TURN != Turn::kNone || normed))
+#pragma unroll
+      for (int i = 0; i < 8; ++i) in.x[i] = (T)x[i];
+    *(Eight<T>*)(dst + e) = in;
+  };
+  // every lane of a wave takes the same number of steps: the exchanges need them all
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (i * groups < vectors) store(u_first + i * groups, ahead[i]);
+  for (int u = AHEAD * groups; u < vectors; u += groups) {
+    Eight<T> x = {};
+    if (u_first + u < vectors) x = source(u_first + u);
+    store(u_first + u, x);
   }
+}
+
+template <typename T>
+void launch(const Paged& P, const AppendArgs& a, unsigned blocks, hipStream_t stream) {
+  const bool norm = a.q_norm || a.k_norm;
+  const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), 0, stream, P, a); };
+  if (!a.cos)
+    norm ? go(append_kernel<T, Turn::kNone, true>) : go(append_kernel<T, Turn::kNone, false>);
+  else if (a.interleaved)
+    norm ? go(append_kernel<T, Turn::kPairs, true>) : go(append_kernel<T, Turn::kPairs, false>);
+  else
+    norm ? go(append_kernel<T, Turn::kHalves, true>) : go(append_kernel<T, Turn::kHalves, false>);
 }
 
 }  // namespace
@@ -171,15 +222,16 @@ extern "C" int grid_kv_append(const grid_paged_cache* cache, const grid_chunks* 
   a.half = g.rot_dim / 2;
   a.interleaved = g.interleaved;
   a.eps = g.eps;
+  a.over = 1.f / (float)D;
   a.lanes = 1;
   while (a.lanes * 8 < D) a.lanes *= 2;
   const Paged P = make_paged(cache, chunks);
   const int blocks = P.T + (g.status ? (P.B + kThreads - 1) / kThreads : 0);
   if (blocks == 0) return GRID_OK;
   if (cache->dtype == GRID_DTYPE_BF16)
-    hipLaunchKernelGGL(append_kernel<bf16_t>, dim3((unsigned)blocks), dim3(kThreads), 0, (hipStream_t)stream, P, a);
+    launch<bf16_t>(P, a, (unsigned)blocks, (hipStream_t)stream);
   else
-    hipLaunchKernelGGL(append_kernel<f16_t>, dim3((unsigned)blocks), dim3(kThreads), 0, (hipStream_t)stream, P, a);
+    launch<f16_t>(P, a, (unsigned)blocks, (hipStream_t)stream);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(GRID_E_HIP, std::string("grid_kv_append launch: ") + hipGetErrorString(e));
   return GRID_OK;

@@ -58,15 +58,15 @@ struct Chunk {
   int32_t first, n, kv;  // first token, new tokens, cached tokens with them
   bool ok;
 };
-__device__ inline Chunk chunk_of(const Paged& P, int b) {
+__device__ inline Chunk chunk_of(const Paged& P, int32_t first, int32_t end, int32_t kv) {
   Chunk c;
-  c.first = P.cu_q[b];
-  const int32_t end = P.cu_q[b + 1];
-  c.kv = P.kv_len[b];
-  c.ok = c.first >= 0 && end >= c.first && end <= P.T;
-  c.n = c.ok ? end - c.first : 0;
-  c.ok = c.ok && c.kv >= c.n && c.kv <= P.reach;
+  c.first = first;
+  c.kv = kv;
+  c.ok = first >= 0 && end >= first && end <= P.T;
+  c.n = c.ok ? end - first : 0;
+  c.ok = c.ok && kv >= c.n && kv <= P.reach;
   return c;
 }
+__device__ inline Chunk chunk_of(const Paged& P, int b) { return chunk_of(P, P.cu_q[b], P.cu_q[b + 1], P.kv_len[b]); }
 
 }  // namespace grid

@@ -12,6 +12,7 @@
 #include <string>
 #include <type_traits>
 
+#include "lanes.h"
 #include "paged.h"
 
 using namespace grid;
@@ -98,32 +99,6 @@ __device__ inline uint32_t bits8(const uint32_t* mask, int t, int V) {
   uint32_t m = mask ? ((const uint8_t*)mask)[t >> 3] : 0xFFu;
   if (t + 8 > V) m &= (1u << (V - t)) - 1u;
   return m;
-}
-
-// Across a wave, by lanes' exchanges that need no LDS: f of all lanes in every lane.
-template <typename F>
-__device__ inline uint32_t across(uint32_t x, F f) {
-  x = f(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xF, 0xF, true));   // lane ^ 1
-  x = f(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true));   // lane ^ 2
-  x = f(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x141, 0xF, 0xF, true));  // 7 - lane, of 8
-  x = f(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x140, 0xF, 0xF, true));  // 15 - lane, of 16
-  auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-  x = f(r[0], r[1]);
-  r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-  return f(r[0], r[1]);
-}
-__device__ inline float max_across(float x) {
-  return __uint_as_float(across(__float_as_uint(x), [](uint32_t p, uint32_t q) {
-    return __float_as_uint(fmaxf(__uint_as_float(p), __uint_as_float(q)));
-  }));
-}
-__device__ inline float sum_across(float x) {
-  return __uint_as_float(across(__float_as_uint(x), [](uint32_t p, uint32_t q) {
-    return __float_as_uint(__uint_as_float(p) + __uint_as_float(q));
-  }));
-}
-__device__ inline int min_across(int x) {
-  return (int)across((uint32_t)x, [](uint32_t p, uint32_t q) { return (uint32_t)min((int)p, (int)q); });
 }
 
 // What is known of some of a row's tokens.  score: the largest w / noise, relative to m as w is; idx: its lowest index,
