@@ -2,21 +2,56 @@
 so it is tested through the C ABI with addresses that are never read."""
 
 import ctypes
+import types
 
 import pytest
 
 AT = 1 << 20  # an address of the right alignment
 
 
+_vp, _i32, _i64, _f32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
+_TWO, _THREE = _i64 * 2, _i64 * 3
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("k_pages", _vp), ("v_pages", _vp), ("dtype", _i32), ("n_pages", _i32), ("page_size", _i32),
+                ("n_kv_heads", _i32), ("head_dim", _i32), ("k_stride", _THREE), ("v_stride", _THREE)]
+
+
+class _Chunks(ctypes.Structure):
+    _fields_ = [("n_seqs", _i32), ("n_tokens", _i32), ("block_table", _vp), ("table_stride", _i64), ("table_cols", _i32),
+                ("kv_len", _vp), ("cu_q", _vp)]
+
+
+class _Append(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("q", _vp), ("q_out", _vp), ("n_heads", _i32), ("k_stride", _TWO),
+                ("v_stride", _TWO), ("q_stride", _TWO), ("q_out_stride", _TWO), ("cos", _vp), ("sin", _vp),
+                ("n_positions", _i32), ("rot_dim", _i32), ("interleaved", _i32), ("q_norm", _vp), ("k_norm", _vp),
+                ("eps", _f32), ("status", _vp)]
+
+
+class _Attend(ctypes.Structure):
+    _fields_ = [("q", _vp), ("out", _vp), ("q_stride", _TWO), ("out_stride", _TWO), ("lse", _vp), ("n_heads", _i32),
+                ("max_q", _i32), ("max_kv", _i32), ("window", _i32), ("scale", _f32), ("workspace", _vp),
+                ("workspace_bytes", _sz)]
+
+
+class _Verify(ctypes.Structure):
+    _fields_ = [("logits", _vp), ("dtype", _i32), ("B", _i32), ("K", _i32), ("V", _i32), ("logits_stride", _TWO),
+                ("mask", _vp), ("mask_stride", _TWO), ("draft", _vp), ("draft_len", _vp), ("draft_probs", _vp),
+                ("probs_stride", _TWO), ("uniform", _vp), ("noise", _vp), ("noise_stride", _i64), ("temperature", _vp),
+                ("tokens", _vp), ("accepted", _vp), ("logprobs", _vp), ("workspace", _vp), ("workspace_bytes", _sz)]
+
+
 @pytest.fixture(scope="module")
 def S():
     pytest.importorskip("torch")
     import paper_2607_11951_amd as pkg
-    if not pkg.grid.LIB_PATH.exists():
+    if not pkg.grid.LIB_PATH.exists() or not (pkg.grid.PKG / "_step.so").exists():
         from paper_2607_11951_amd import build
         build.build()
-    from paper_2607_11951_amd import step
-    return step
+    return types.SimpleNamespace(lib=pkg.lib, G=pkg, _Cache=_Cache, _Chunks=_Chunks, _Append=_Append, _Attend=_Attend,
+                                 _Verify=_Verify, _TWO=_TWO, _THREE=_THREE)
 
 
 def cache(S, **kw):
@@ -159,24 +194,74 @@ def test_workspace_sizes(S):
 
 
 def test_python_refusals(S):
+    """wrong types, shapes, layouts and devices, through the package's functions: on tensors in host memory everything
+    else is checked before their device is"""
     torch = pytest.importorskip("torch")
-    k = torch.zeros(4, 16, 2, 64, dtype=torch.bfloat16)
-    with pytest.raises(ValueError):
-        S._paged(k, k[:, :, :1])
-    with pytest.raises(ValueError):
-        S._paged(k.transpose(2, 3), k.transpose(2, 3))
-    with pytest.raises(TypeError):
-        S._paged(k.float(), k.float())
-    table, one = torch.zeros(3, 5, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
-    four = torch.zeros(4, dtype=torch.int32)
-    S._chunks(7, table, one, four, k.device)
-    for t, n, c in [(table.long(), one, four), (table[0], one, four), (table, four, four), (table, one, one),
-                    (table, one.long(), four), (table.T, one, four)]:
-        with pytest.raises(ValueError):
-            S._chunks(7, t, n, c, k.device)
-    with pytest.raises(ValueError):
-        S._vectors(torch.zeros(7, 2, 64), torch.bfloat16, 7, 64, k.device, "q")
-    with pytest.raises(ValueError):
-        S._vectors(torch.zeros(7, 2, 64).transpose(1, 2), torch.float32, 7, 2, k.device, "q")
-    with pytest.raises(TypeError):
-        S.verify(torch.zeros(1, 2, 8, dtype=torch.float64), four[:1].view(1, 1))
+    half, zeros = torch.bfloat16, torch.zeros
+    pages = zeros(4, 16, 2, 64, dtype=half)
+    table, lens, cu = zeros(3, 5, dtype=torch.int32), zeros(3, dtype=torch.int32), zeros(4, dtype=torch.int32)
+    k, q = zeros(7, 2, 64, dtype=half), zeros(7, 6, 64, dtype=half)
+
+    def append(**kw):
+        a = dict(k=k, v=k, k_pages=pages, v_pages=pages, block_table=table, kv_len=lens, cu_q=cu, q=q)
+        S.G.kv_append(**{**a, **kw})
+
+    def attend(**kw):
+        a = dict(q=q, k_pages=pages, v_pages=pages, block_table=table, kv_len=lens, cu_q=cu, max_q=7, max_kv=80)
+        S.G.attend(**{**a, **kw})
+
+    def refused(call, error, word, **kw):
+        with pytest.raises(error, match=word):
+            call(**kw)
+
+    for call in (append, attend):
+        refused(call, ValueError, "GPU")  # nothing else is wrong
+        refused(call, ValueError, "alike", v_pages=pages[:, :, :1])
+        refused(call, ValueError, "alike", v_pages=pages.half())
+        refused(call, ValueError, "dense", k_pages=pages.transpose(2, 3), v_pages=pages.transpose(2, 3))
+        refused(call, TypeError, "bfloat16", k_pages=pages.float(), v_pages=pages.float())
+        refused(call, TypeError, "tensor", k_pages=None)
+        refused(call, ValueError, "block_table", block_table=table.long())
+        refused(call, ValueError, "block_table", block_table=table[0])
+        refused(call, ValueError, "block_table", block_table=table.T)
+        refused(call, ValueError, "kv_len", kv_len=cu)
+        refused(call, ValueError, "kv_len", kv_len=lens.long())
+        refused(call, ValueError, "cu_q", cu_q=lens)
+    for bad in (k.float(), k[:, :, :32], k[:5], k[0], zeros(7, 64, 2, dtype=half).transpose(1, 2)):
+        refused(append, ValueError, "v: ", v=bad)
+        refused(attend, ValueError, "q: ", q=bad) if bad.shape[0] == 7 else None
+    refused(append, ValueError, "heads", k=q, v=q)
+    table_f = zeros(9, 32)
+    refused(append, ValueError, "together", cos=table_f)
+    refused(append, ValueError, "cos", cos=table_f.double(), sin=table_f)
+    refused(append, ValueError, "sin", cos=table_f, sin=table_f[:5])
+    refused(append, ValueError, "q_norm", q_norm=zeros(32))
+    refused(append, ValueError, "k_norm", k_norm=zeros(64, dtype=half))
+    refused(append, ValueError, "status", status=zeros(3))
+    refused(append, TypeError, "eps", eps="x")
+    refused(attend, ValueError, "lse", lse=zeros(7, 5))
+    refused(attend, TypeError, "max_q", max_q=1.5)
+    refused(attend, TypeError, "max_kv", max_kv=None)
+    refused(attend, TypeError, "scale", scale="x")
+
+    draft, logits = zeros(2, 3, dtype=torch.int32), zeros(2, 4, 40)
+
+    def verify(**kw):
+        S.G.verify(**{**dict(logits=logits, draft=draft), **kw})
+
+    refused(verify, ValueError, "GPU")
+    refused(verify, TypeError, "float32", logits=logits.double())
+    refused(verify, ValueError, "logits", logits=logits[0])
+    refused(verify, ValueError, "logits", logits=zeros(2, 40, 4).transpose(1, 2))
+    refused(verify, ValueError, "draft", draft=draft.long())
+    refused(verify, ValueError, "draft", draft=draft[:, :2])
+    refused(verify, ValueError, "draft_len", draft_len=zeros(3, dtype=torch.int32))
+    refused(verify, ValueError, "mask", mask=zeros(2, 4, 1, dtype=torch.int32))
+    refused(verify, ValueError, "mask", mask=zeros(2, 3, 2, dtype=torch.int32))
+    refused(verify, ValueError, "draft_probs", draft_probs=zeros(2, 4, 40))
+    refused(verify, ValueError, "uniform", uniform=zeros(2, 4))
+    refused(verify, ValueError, "noise", noise=zeros(2, 39))
+    refused(verify, ValueError, "temperature", temperature=zeros(1))
+    refused(verify, ValueError, "tokens", tokens=zeros(2, 4))
+    refused(verify, ValueError, "accepted", accepted=zeros(3, dtype=torch.int32))
+    refused(verify, ValueError, "logprobs", logprobs=zeros(2, 3))
