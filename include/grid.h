@@ -599,7 +599,7 @@ typedef struct {
   int32_t n_tokens;            /* rows of the packed arrays, 0 .. 2^24 */
   const int32_t* block_table;  /* device [B][table_stride] */
   int64_t table_stride;        /* >= table_cols */
-  int32_t table_cols;          /* >= 1, table_cols * page_size < 2^31 */
+  int32_t table_cols;          /* >= 1, table_cols * page_size < 2^31 - 4096 */
   const int32_t* kv_len;       /* device [B] */
   const int32_t* cu_q;         /* device [B + 1] */
 } grid_chunks;
@@ -618,7 +618,7 @@ typedef struct {
   const void* q;           /* or NULL: no queries */
   void* q_out;             /* may be q (same strides) */
   int32_t n_heads;         /* query heads (with q) */
-  int64_t k_stride[2];     /* token, head; in elements, multiples of 8; 16-byte aligned */
+  int64_t k_stride[2];     /* token, head; in elements, multiples of 8 below 2^31; 16-byte aligned */
   int64_t v_stride[2];
   int64_t q_stride[2];
   int64_t q_out_stride[2];
@@ -656,7 +656,7 @@ int grid_kv_append(const grid_paged_cache* cache, const grid_chunks* chunks, con
 typedef struct {
   const void* q;           /* device [n_tokens], the cache's dtype */
   void* out;
-  int64_t q_stride[2];     /* token, head; in elements, multiples of 8; 16-byte aligned */
+  int64_t q_stride[2];     /* token, head; in elements, multiples of 8 below 2^31; 16-byte aligned */
   int64_t out_stride[2];
   float* lse;              /* device [n_tokens][n_heads] or NULL */
   int32_t n_heads;         /* a multiple of n_kv_heads, at most 1024 */

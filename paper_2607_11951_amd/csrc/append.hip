@@ -151,8 +151,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Paged P, AppendArgs a)
     }
     if (u >= vectors) return;
     const int h = key ? u : value ? u - P.hkv : u - 2 * P.hkv;
-    uint16_t* dst = key ? P.k + page * P.ks[0] + row * P.ks[1] + h * P.ks[2]
-                    : value ? P.v + page * P.vs[0] + row * P.vs[1] + h * P.vs[2] : a.qout + t * a.os[0] + h * a.os[1];
+    uint16_t* dst = key ? P.k + P.at(P.ks, page, row) + (uint64_t)h * P.ks[2]
+                    : value ? P.v + P.at(P.vs, page, row) + (uint64_t)h * P.vs[2] : a.qout + t * a.os[0] + h * a.os[1];
     if (!value && (TURN != Turn::kNone || normed))
 #pragma unroll
       for (int i = 0; i < 8; ++i) in.x[i] = (T)x[i];

@@ -46,7 +46,7 @@ struct Vec<f16_t> {
 struct AttendArgs {
   const uint16_t* q;
   uint16_t* out;
-  int64_t qs[2], os[2];
+  uint32_t qs[2], os[2];  // token, head
   float* lse;
   float2* part_ml;  // [slots][rows of a tile]: maximum (in base 2 units of the scaled score), sum
   float* part_o;    // [slots][rows of a tile][D], not divided by the sum
@@ -56,6 +56,10 @@ struct AttendArgs {
   int32_t tiles, splits, len;  // many rows: tiles a sequence, ranges of len keys (a multiple of the stage)
   float c;                     // |scale| * log2 e, above 0
   bool negate;                 // scale < 0: the queries are negated
+
+  static __device__ uint64_t at(const uint32_t* stride, int t, int h) {
+    return (uint64_t)t * stride[0] + (uint64_t)h * stride[1];
+  }
 };
 
 constexpr float kLn2 = 0.693147180559945309417f, kLog2e = 1.44269504088896340736f;
@@ -96,11 +100,13 @@ __device__ constexpr int swz(int row) {
   return D == 64 ? ((row >> 1 & 1) << 2 | (row >> 2 & 3)) : ((row & 3) << 2 | (row >> 2 & 3));
 }
 
-// The keys whose values were cleaned: first, and after the last.
+// What a workgroup notes in LDS on its way: the keys whose values were cleaned (first, and after the last), and whether
+// a page was not in the cache.
 __device__ inline void no_fix(int* fix) {
   if (threadIdx.x == 0) {
     fix[0] = INT32_MAX;
     fix[1] = 0;
+    fix[2] = 0;
   }
 }
 
@@ -153,7 +159,7 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
   // Loads.  Load i of a wave brings RPI rows from row WR * wave + i * RPI of the stage on, a lane piece `lane % PR` of
   // row `lane / PR`; rows at and after s_hi are the last row again.
   const uint32_t base = (uint32_t)(uintptr_t)(GRID_LDS uint8_t*)lds;
-  const uint16_t *kg = P.k + g * P.ks[2], *vg = P.v + g * P.vs[2];
+  const uint16_t *kg = P.k + (uint64_t)g * P.ks[2], *vg = P.v + (uint64_t)g * P.vs[2];
   const auto* table = (const __attribute__((address_space(4))) int32_t*)(P.table + (int64_t)b * P.table_stride);
   const int lrow = lane / PR;
   constexpr int FIND = UNI ? RUNS : LOADS;
@@ -176,28 +182,31 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
       page[i] = in ? page[i] : 0;
     }
   };
-  const auto fetch = [&](const uint16_t* x, const int64_t* st, int s0, uint32_t to) {
+  const auto fetch = [&](const uint16_t* x, const uint32_t* st, int s0, uint32_t to) {
     to += (uint32_t)(wave * WR * D * 2);
+    const uint32_t step = lrow * st[1];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int piece = lane % PR ^ swz<D>(wave * WR + i * RPI + lrow);
       if constexpr (UNI) {
         constexpr int PER = RUN / RPI;
-        const int f = i / PER, s = s0 + wave * WR + f * RUN;
-        const uint16_t* p = x + (uint64_t)(uint32_t)page[f] * (uint32_t)st[0] + (uint64_t)row[f] * (uint32_t)st[1];
+        const int f = i / PER, s = s0 + wave * WR + f * RUN, before = i % PER * RPI;
+        // (scalars, whatever registers they were kept in)
+        const int pg = __builtin_amdgcn_readfirstlane(page[f]);
+        const uint32_t r = (uint32_t)__builtin_amdgcn_readfirstlane((int)row[f]);
         const int last = s_hi - 1 - min(s, (s_hi - 1) & ~(RUN - 1));  // last row of the run to read
-        const uint32_t rr = (uint32_t)min(i % PER * RPI + lrow, last);
-        to_lds(p, (rr * (uint32_t)st[1] + piece * 8) * 2, to + i * 1024);
+        const uint16_t* p = x + P.at(st, pg, r + (uint32_t)min(before, last));
+        const uint32_t lr = last >= RUN - 1 ? step : (uint32_t)min(lrow, max(last - before, 0)) * st[1];
+        to_lds(p, (lr + piece * 8) * 2, to + i * 1024);
       } else {
-        to_lds(x + (uint64_t)(uint32_t)page[i] * (uint32_t)st[0] + (uint64_t)row[i] * (uint32_t)st[1] + piece * 8,
-               to + i * 1024);
+        to_lds(x + P.at(st, page[i], row[i]) + piece * 8, to + i * 1024);
       }
     }
   };
 
   Eight q[QS];
   const auto load_q = [&] {
-    const uint16_t* src = a.q + qt * a.qs[0] + qh * a.qs[1] + half * 8;
+    const uint16_t* src = a.q + a.at(a.qs, qt, qh) + half * 8;
     const uint32_t flip = a.negate ? 0x80008000u : 0u;
 #pragma unroll
     for (int k = 0; k < QS; ++k) {
@@ -330,10 +339,10 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
     }
     for (int s0 = s_lo; s0 + kw * KT < s_hi; s0 += SK) {
       const int k0 = s0 + kw * KT;
-      const bool more = k0 + SK < s_hi, seen = k0 <= pos_max && (!a.window || k0 + KT > pos_min - a.window + 1);
+      const bool more = k0 + SK < s_hi;
       if (more) find(s0 + SK);
       wait_loads<LOADS>();
-      if (seen) scores(ks);
+      scores(ks);
       wait_reads();
       if (more) {
         fetch(kg, P.ks, s0 + SK, base);
@@ -341,14 +350,12 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
       } else {
         wait_loads<0>();
       }
-      if (seen) {
-        if (masked(k0)) {
-          mask(k0);
-          clean(base + kHalf, s0);
-        }
-        softmax();
-        sums(vs);
+      if (masked(k0)) {
+        mask(k0);
+        clean(base + kHalf, s0);
       }
+      softmax();
+      sums(vs);
       wait_reads();
       if (more) fetch(vg, P.vs, s0 + SK, base + kHalf);
     }
@@ -383,14 +390,16 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
         sums(vs);
       }
       buf ^= 2 * kHalf;
+      wait_reads();
       wait_loads<0>();
       if (s0 + SK < s_hi && torn(s0 + SK)) clean(base + buf + kHalf, s0 + SK);
       __syncthreads();
     }
   }
   l += other_half(l);
-  missing = __syncthreads_or(missing);
-  if (missing) l = NAN;
+  if (missing) fix[2] = 1;
+  __syncthreads();
+  if (fix[2]) l = NAN;
   float mc = m * a.c;  // -inf where the row saw nothing
 
   // adds to four sums of the row at position p the values that were taken out and that it sees
@@ -402,7 +411,7 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
       const int id = P.page_of(b, (uint32_t)s, rr);
       if (!P.in_cache(id)) continue;
       T y[4];
-      __builtin_memcpy(y, vg + (uint64_t)(uint32_t)id * (uint32_t)P.vs[0] + (uint64_t)rr * (uint32_t)P.vs[1] + e, 8);
+      __builtin_memcpy(y, vg + P.at(P.vs, id, rr) + e, 8);
       const float f[4] = {(float)y[0], (float)y[1], (float)y[2], (float)y[3]};
       x.x += __builtin_isfinite(f[0]) ? 0.f : f[0];
       x.y += __builtin_isfinite(f[1]) ? 0.f : f[1];
@@ -414,39 +423,20 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
   // waves that took other keys of the same rows: their sums meet in LDS
   if constexpr (KW > 1) {
     constexpr int DH = D / 2;                     // in two halves of the entries, for room
-    float* ml = (float*)lds;                      // [KW][2][TM]
+    float2* ml = (float2*)lds;                    // [KW][TM]
     float* os = (float*)(lds + KW * 2 * TM * 4);  // [KW][TM][DH + 4]
-    if (half == 0) {
-      ml[(kw * 2 + 0) * TM + rw * 32 + col] = mc;
-      ml[(kw * 2 + 1) * TM + rw * 32 + col] = l;
-    }
-    __syncthreads();
-    float top = -INFINITY, sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < KW; ++w) top = fmaxf(top, ml[w * 2 * TM + rw * 32 + col]);
-    const float ref = top == -INFINITY ? 0.f : top;
-#pragma unroll
-    for (int w = 0; w < KW; ++w)
-      sum += ml[(w * 2 + 1) * TM + rw * 32 + col] * __builtin_amdgcn_exp2f(ml[w * 2 * TM + rw * 32 + col] - ref);
-    const float keep = __builtin_amdgcn_exp2f(mc - ref);
-    mc = top;
-    l = sum;
-    __syncthreads();
-    if (kw == 0 && half == 0) {
-      ml[rw * 32 + col] = mc;
-      ml[TM + rw * 32 + col] = l;
-    }
+    if (half == 0) ml[kw * TM + rw * 32 + col] = make_float2(mc, l);
     float* mine = os + (kw * TM + rw * 32 + col) * (DH + 4);
     constexpr int PART = 32 * DH / 4 / 64 / KW;  // float4s a lane
 #pragma unroll
     for (int hd = 0; hd < 2; ++hd) {
+      if (hd > 0) __syncthreads();
 #pragma unroll
       for (int d = 0; d < DB / 2; ++d)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
           const float16_v& x = o[hd * (DB / 2) + d];
-          *(float4*)(mine + d * 32 + 2 * i + 4 * half) =
-              make_float4(x[i] * keep, x[i + 1] * keep, x[i + 2] * keep, x[i + 3] * keep);
+          *(float4*)(mine + d * 32 + 2 * i + 4 * half) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
         }
       __syncthreads();
       // a wave adds up a part of its rows' entries
@@ -454,32 +444,37 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
       for (int j = 0; j < PART; ++j) {
         const int at = (j * KW + kw) * 64 + lane, rr = rw * 32 + at / (DH / 4), e = at % (DH / 4) * 4;
         if (tile * TM + rr >= rows) continue;
+        float rm = -INFINITY, rl = 0.f;
+#pragma unroll
+        for (int w = 0; w < KW; ++w) rm = fmaxf(rm, ml[w * TM + rr].x);
+        const float ref = rm == -INFINITY ? 0.f : rm;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < KW; ++w) {
+          const float2 p = ml[w * TM + rr];
+          const float f = __builtin_amdgcn_exp2f(p.x - ref);
           const float4 y = *(const float4*)(os + (w * TM + rr) * (DH + 4) + e);
-          x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
+          rl += p.y * f;
+          x.x += y.x * f, x.y += y.y * f, x.z += y.z * f, x.w += y.w * f;
         }
         const int i = (int)a.group.quot((uint32_t)(tile * TM + rr)), h = g * G + tile * TM + rr - i * G, t = ch.first + i;
-        const float rm = ml[rr], rl = ml[TM + rr];
         settle(x, first_pos + i, hd * DH + e);
         if (whole) {
           const float over = rl == 0.f ? 0.f : 1.f / rl;
           T y[4] = {(T)(x.x * over), (T)(x.y * over), (T)(x.z * over), (T)(x.w * over)};
-          *(uint2*)(a.out + t * a.os[0] + h * a.os[1] + hd * DH + e) = *(uint2*)y;
+          *(uint2*)(a.out + a.at(a.os, t, h) + hd * DH + e) = *(uint2*)y;
           if (a.lse && e == 0 && hd == 0) a.lse[(int64_t)t * a.hq + h] = (rm + __builtin_amdgcn_logf(rl)) * kLn2;
         } else {
           *(float4*)(a.part_o + (slot * TM + rr) * D + hd * DH + e) = x;
           if (e == 0 && hd == 0) a.part_ml[slot * TM + rr] = make_float2(rm, rl);
         }
       }
-      if (hd == 0) __syncthreads();
     }
   } else {
     if (r0 + col >= rows) return;
     if (whole) {
       const float over = l == 0.f ? 0.f : 1.f / l;
-      uint16_t* dst = a.out + qt * a.os[0] + qh * a.os[1] + 4 * half;
+      uint16_t* dst = a.out + a.at(a.os, qt, qh) + 4 * half;
 #pragma unroll
       for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -513,7 +508,7 @@ __device__ void fill_nan(const Paged& P, const AttendArgs& a, const Chunk& ch, i
   const int from = min(max(ch.first, 0), P.T), to = min(max(P.cu_q[b + 1], from), P.T);
   for (int64_t i = threadIdx.x; i < (int64_t)(to - from) * a.hq * D; i += nt) {
     const int t = from + (int)(i / (a.hq * D)), e = (int)(i % (a.hq * D));
-    ((T*)a.out)[t * a.os[0] + (e / D) * a.os[1] + e % D] = (T)NAN;
+    ((T*)a.out)[a.at(a.os, t, e / D) + e % D] = (T)NAN;
     if (a.lse && e % D == 0) a.lse[(int64_t)t * a.hq + e / D] = NAN;
   }
 }
@@ -522,7 +517,7 @@ __device__ void fill_nan(const Paged& P, const AttendArgs& a, const Chunk& ch, i
 template <typename T, typename X>
 __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void tiles_kernel(Paged P, AttendArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[X::kLds];
-  __shared__ int fix[2];
+  __shared__ int fix[3];
   no_fix(fix);
   __syncthreads();
   uint32_t id = blockIdx.x;
@@ -549,6 +544,18 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void tiles_kernel(Paged P
          (((int64_t)b * P.hkv + g) * a.tiles + tile) * a.splits + split);
 }
 
+__device__ inline uint64_t uniform(uint64_t x) {  // the same in all lanes: known to be
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 |
+         (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+}
+
+// floor(i * total / n) and floor(i * n / total), i <= total, n <= 2^9: in 32 bits where they fit, as they do but for caches
+// of a thousand million positions.
+__device__ inline uint64_t scaled(uint64_t i, uint64_t by, uint64_t over, uint64_t total) {
+  if (total < 1u << 22) return (uint32_t)(i * by) / (uint32_t)over;
+  return i * by / over;
+}
+
 // Few rows: every sequence's rows are one tile, and the work is the stages of all sequences and key heads in a row,
 // cut into equal shares: workgroup i takes stages i * total / n .. (i + 1) * total / n - 1, whatever units they belong
 // to.  So all finish together, however ragged the lengths.  Of a unit that workgroups share, the sums of the one that
@@ -556,104 +563,157 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void tiles_kernel(Paged P
 template <typename T, typename X>
 __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void shares_kernel(Paged P, AttendArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[X::kLds];
-  __shared__ uint64_t waves[X::W], found[2];
-  __shared__ int fix[2];
+  __shared__ uint64_t waves[X::W], found[2], kept[4];
+  __shared__ int fix[3];
   no_fix(fix);
   const int tid = (int)threadIdx.x, lane = tid & 63;
   const uint64_t me = blockIdx.x, heads = (uint64_t)P.hkv;
   const auto stages = [&](const Chunk& c) {
     return is_bad(a, c) || c.n == 0 ? 0u : (uint32_t)((c.kv - first_key(a, c) + X::SK - 1) / X::SK);
   };
-  // stages of the sequences before a thread's: each thread adds up a run of sequences
-  const int per = (P.B + X::NT - 1) / X::NT, b0 = min(tid * per, P.B), b1 = min(b0 + per, P.B);
+  const bool few = P.B <= 64;  // sequences: a lane each, in every wave; otherwise a run of them each thread
+  const int per = few ? 1 : (P.B + X::NT - 1) / X::NT, b0 = min((few ? lane : tid) * per, P.B), b1 = min(b0 + per, P.B);
+  Chunk own = {0, 0, 0, false};
   uint64_t mine = 0;
-  for (int b = b0; b < b1; ++b) mine += stages(chunk_of(P, b));
-  uint64_t upto = mine;
+  for (int b = b0; b < b1; ++b) {
+    own = chunk_of(P, b);
+    mine += stages(own);
+  }
+  uint64_t upto = mine;  // with the stages of the sequences before
   for (int o = 1; o < 64; o <<= 1) {
     const uint64_t x = __shfl_up((unsigned long long)upto, o);
     if (lane >= o) upto += x;
   }
-  if (lane == 63) waves[tid >> 6] = upto;
-  __syncthreads();
-  uint64_t total = 0;
-  for (int w = 0; w < X::W; ++w) {
-    if (w < tid >> 6) upto += waves[w];
-    total += waves[w];
-  }
-  total *= heads;
-  for (int b = (int)me; b < P.B; b += (int)gridDim.x) {
-    const Chunk c = chunk_of(P, b);
-    if (is_bad(a, c)) fill_nan<T, X::D>(P, a, c, b, X::NT);
-  }
-  const uint64_t n = min((uint64_t)gridDim.x, total);  // no share is empty
-  if (me >= n) return;
-  uint64_t x = me * total / n;
-  const uint64_t end = (me + 1) * total / n;
-  if (x >= (upto - mine) * heads && x < upto * heads) {
-    uint64_t before = upto - mine;
-    int b = b0;
-    for (; b < b1 - 1; ++b) {
-      const uint32_t s = stages(chunk_of(P, b));
-      if (x < (before + s) * heads) break;
-      before += s;
+  uint64_t total;
+  if (few) {
+    total = __shfl((unsigned long long)upto, 63);
+  } else {
+    if (lane == 63) waves[tid >> 6] = upto;
+    __syncthreads();
+    total = 0;
+    for (int w = 0; w < X::W; ++w) {
+      if (w < tid >> 6) upto += waves[w];
+      total += waves[w];
     }
-    found[0] = (uint64_t)b;
-    found[1] = before;
   }
-  __syncthreads();
-  int b = (int)found[0];
-  uint64_t first = found[1] * heads;  // stages before sequence b
-  b = __builtin_amdgcn_readfirstlane(b);
-  while (x < end) {
-    const Chunk ch = chunk_of(P, b);
+  total = uniform(total * heads);
+  if (few ? __any(b0 < b1 && is_bad(a, own)) : true)
+    for (int b = (int)me; b < P.B; b += (int)gridDim.x) {
+      const Chunk c = chunk_of(P, b);
+      if (is_bad(a, c)) fill_nan<T, X::D>(P, a, c, b, X::NT);
+    }
+  uint64_t n = min((uint64_t)gridDim.x, total);  // no share is empty
+  if (me >= n) return;
+  uint64_t x = uniform(scaled(total, me, n, total));
+  uint64_t end = uniform(scaled(total, me + 1, n, total));
+  const bool here = x >= (upto - mine) * heads && x < upto * heads;
+  int b;
+  uint64_t first;  // stages before sequence b
+  Chunk ch;
+  if (few) {
+    b = __builtin_ctzll(__ballot(here));
+    first = uniform(__shfl((unsigned long long)(upto - mine), b)) * heads;
+    ch.first = __builtin_amdgcn_readlane(own.first, b);
+    ch.n = __builtin_amdgcn_readlane(own.n, b);
+    ch.kv = __builtin_amdgcn_readlane(own.kv, b);
+    ch.ok = true;
+    __syncthreads();  // no_fix
+  } else {
+    if (here) {
+      uint64_t before = upto - mine;
+      int i = b0;
+      for (; i < b1 - 1; ++i) {
+        const uint32_t s = stages(chunk_of(P, i));
+        if (x < (before + s) * heads) break;
+        before += s;
+      }
+      found[0] = (uint64_t)i;
+      found[1] = before;
+    }
+    __syncthreads();
+    b = __builtin_amdgcn_readfirstlane((int)found[0]);
+    first = uniform(found[1]) * heads;
+    ch = chunk_of(P, b);
+  }
+  for (;;) {
     const uint64_t s = stages(ch);
     if (x >= first + s * heads) {  // the next sequence (b < P.B: x < end <= total)
       first += s * heads;
-      ++b;
+      ch = chunk_of(P, ++b);
       continue;
     }
     const int g = __builtin_amdgcn_readfirstlane((int)((uint32_t)(x - first) / (uint32_t)s));
     const uint64_t unit = first + (uint64_t)g * s, stop = min(end, unit + s);
     const bool whole = x == unit && stop == unit + s;
     if (x == unit && tid == 0)
-      a.runs[(int64_t)b * P.hkv + g] = make_int2((int)me, (int)(((unit + s) * n - 1) / total));
+      a.runs[(int64_t)b * P.hkv + g] =
+          make_int2((int)me, whole ? (int)me : (int)(((unit + s) * n - 1) / total));
     const int start = first_key(a, ch);
     const int s_lo = __builtin_amdgcn_readfirstlane(start + (int)(x - unit) * X::SK);
     const int s_hi = __builtin_amdgcn_readfirstlane(min(ch.kv, start + (int)(stop - unit) * X::SK));
+    // what the loop goes on with waits in LDS: the stages need the scalar registers
+    if (tid == 0) {
+      kept[0] = stop;
+      kept[1] = end;
+      kept[2] = first;
+      kept[3] = total;
+    }
     X::run(P, a, lds, fix, ch, b, g, 0, s_lo, s_hi, whole, (int64_t)me * 2 + (x == unit));
-    x = stop;
-    if (x >= end) break;
+    x = uniform(kept[0]);
+    end = uniform(kept[1]);
+    if (x >= end) return;
+    first = uniform(kept[2]);
+    total = uniform(kept[3]);
+    n = min((uint64_t)gridDim.x, total);
     __syncthreads();
     no_fix(fix);
     __syncthreads();
   }
 }
 
-// The parts of a row joined: a workgroup a token and head, D / 4 lanes a part, several parts side by side.
-template <typename T, int D, int TM, bool SHARES>
+// The parts of a row (a token and head) joined by WAVES waves: D / 4 lanes a part, several parts side by side.
+template <typename T, int D, int TM, bool SHARES, int WAVES>
 __global__ __launch_bounds__(256) void join_kernel(Paged P, AttendArgs a) {
-  constexpr int L = D / 4, N = 256 / L;
-  const int tid = (int)threadIdx.x, lane = tid & 63, e = tid % L * 4, side = tid / L;
-  const int t = (int)(blockIdx.x / (uint32_t)a.hq), h = (int)(blockIdx.x % (uint32_t)a.hq);
+  constexpr int L = D / 4, N = 64 * WAVES / L, R = 4 / WAVES;  // lanes a part, parts side by side, rows a workgroup
+  const int tid = (int)threadIdx.x, lane = tid & 63, in = tid % (64 * WAVES), e = in % L * 4, side = in / L;
+  const uint32_t u = blockIdx.x * R + (uint32_t)tid / (64 * WAVES);
+  const int t = (int)(u / (uint32_t)a.hq), h = (int)(u % (uint32_t)a.hq);
+  bool live = t < P.T;
+  // the token's sequence; the lanes hold those of 64 and the one that is found hands its own out
+  Chunk ch = {0, 0, 0, false};
   int b = 0;
-  for (int s = 0; s < P.B; s += 64) b += __popcll(__ballot(s + lane < P.B && P.cu_q[s + lane + 1] <= t));
-  if (b >= P.B) return;
-  const Chunk ch = chunk_of(P, b);
-  if (is_bad(a, ch) || t < ch.first || t >= ch.first + ch.n) return;
+  for (int s = 0; s < P.B; s += 64) {
+    const int x = min(s + lane, P.B - 1);
+    const int32_t first = P.cu_q[x], end = P.cu_q[x + 1], kv = P.kv_len[x];
+    const int before = __popcll(__ballot(s + lane < P.B && end <= t));
+    b += before;
+    if (before < min(64, P.B - s)) {
+      ch = chunk_of(P, __builtin_amdgcn_readlane(first, before), __builtin_amdgcn_readlane(end, before),
+                    __builtin_amdgcn_readlane(kv, before));
+      break;
+    }
+  }
+  live = live && !is_bad(a, ch) && t >= ch.first && t < ch.first + ch.n;
   const int G = (int)a.group.d, g = (int)a.group.quot((uint32_t)h), r = (t - ch.first) * G + h - g * G;
-  int from, to;
+  int from = 0, to = -1;
   int64_t slots = 0;
-  if constexpr (SHARES) {
-    const int2 run = a.runs[(int64_t)b * P.hkv + g];
-    from = run.x;
-    to = run.y;
-    if (from == to) return;
-  } else {
-    const int start = first_key(a, ch), pos = ch.kv - ch.n + t - ch.first;
-    if (ch.kv - start <= a.len) return;
-    from = (max(a.window ? pos - a.window + 1 : 0, start) - start) / a.len;
-    to = (pos - start) / a.len;
-    slots = (((int64_t)b * P.hkv + g) * a.tiles + r / TM) * a.splits;
+  if (live) {
+    if constexpr (SHARES) {
+      const int2 run = a.runs[(int64_t)b * P.hkv + g];
+      from = run.x;
+      to = run.y;
+      live = from != to;
+    } else {
+      const int start = first_key(a, ch), pos = ch.kv - ch.n + t - ch.first;
+      live = ch.kv - start > a.len;
+      from = (max(a.window ? pos - a.window + 1 : 0, start) - start) / a.len;
+      to = (pos - start) / a.len;
+      slots = (((int64_t)b * P.hkv + g) * a.tiles + r / TM) * a.splits;
+    }
+  }
+  if (!live) {
+    if constexpr (WAVES > 1) return;  // the whole workgroup
+    to = from - 1;
   }
   float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -671,18 +731,27 @@ __global__ __launch_bounds__(256) void join_kernel(Paged P, AttendArgs a) {
     const float2 p = a.part_ml[at];
     take(p.x, p.y, *(const float4*)(a.part_o + at * D + e));
   }
-  __shared__ float2 ml[N];
-  __shared__ float4 os[N][L];
-  if (e == 0) ml[side] = make_float2(m, l);
-  os[side][tid % L] = o;
-  __syncthreads();
-  if (side > 0) return;
+  // the sides of a wave, then the waves
 #pragma unroll
-  for (int i = 1; i < N; ++i) take(ml[i].x, ml[i].y, os[i][tid]);
+  for (int d = L; d < 64; d <<= 1) {
+    const float om = __shfl_xor(m, d), ol = __shfl_xor(l, d);
+    take(om, ol, make_float4(__shfl_xor(o.x, d), __shfl_xor(o.y, d), __shfl_xor(o.z, d), __shfl_xor(o.w, d)));
+  }
+  if constexpr (WAVES > 1) {
+    __shared__ float2 ml[WAVES];
+    __shared__ float4 os[WAVES][L];
+    if (lane == 0) ml[tid >> 6] = make_float2(m, l);
+    if (lane < L) os[tid >> 6][lane] = o;
+    __syncthreads();
+    if (tid >= L) return;
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) take(ml[i].x, ml[i].y, os[i][tid]);
+  }
+  if (!live || side > 0) return;
   const float over = l == 0.f ? 0.f : 1.f / l;
   T y[4] = {(T)(o.x * over), (T)(o.y * over), (T)(o.z * over), (T)(o.w * over)};
-  *(uint2*)(a.out + t * a.os[0] + h * a.os[1] + e) = *(uint2*)y;
-  if (a.lse && tid == 0) a.lse[(int64_t)t * a.hq + h] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+  *(uint2*)(a.out + a.at(a.os, t, h) + e) = *(uint2*)y;
+  if (a.lse && e == 0) a.lse[(int64_t)t * a.hq + h] = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 int check(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_attend_args* g, bool pointers) {
@@ -696,6 +765,8 @@ int check(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_a
     return bad("n_heads is a multiple of the key heads, at most 1024");
   if (g->max_q < 1 || g->max_kv < 1 || g->window < 0) return bad("max_q, max_kv or window");
   if (!std::isfinite(g->scale)) return bad("scale");
+  if ((int64_t)std::min(g->max_q, chunks->n_tokens) * (g->n_heads / cache->n_kv_heads) >= 1 << 30)
+    return fail(GRID_E_CAPACITY, "grid_attend: 2^30 rows of a sequence and key head or more");
   if (!pointers || chunks->n_tokens == 0) return GRID_OK;
   if (!g->q || !g->out) return bad("null pointer");
   if (!rows_fit(g->q, g->q_stride, 2) || !rows_fit(g->out, g->out_stride, 2))
@@ -712,7 +783,8 @@ struct Shape {
   int tm, splits, len;
   int64_t tiles, blocks;
   bool join;
-  size_t slots;  // of parts
+  int64_t parts;  // of a row, at most but for one or two
+  size_t slots;   // of parts
 };
 Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_attend_args* g) {
   Shape s;
@@ -729,6 +801,7 @@ Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_atten
     const int64_t stage = 64, stages = (span + stage - 1) / stage;
     s.blocks = std::min<int64_t>(heads * stages, 2 * kComputeUnits);
     s.join = stages > 1;
+    s.parts = s.blocks / heads;
     s.slots = (size_t)s.blocks * 2;
     return s;
   }
@@ -743,6 +816,7 @@ Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_atten
     }
   }
   s.join = s.splits > 1;
+  s.parts = s.splits;
   s.slots = s.join ? (size_t)s.blocks : 0;
   return s;
 }
@@ -756,7 +830,7 @@ size_t workspace_of(const grid_paged_cache* c, const grid_chunks* x, const Shape
 
 template <typename T, int D, int RW, int KW, int KT, int WGS>
 void launch(const Paged& P, const AttendArgs& a, const Shape& s, hipStream_t stream) {
-  const dim3 blocks((unsigned)s.blocks), rows((unsigned)P.T * (unsigned)a.hq);
+  const dim3 blocks((unsigned)s.blocks);
   constexpr bool SHARES = RW * 32 < 128;
   const auto go = [&](auto tile) {
     using X = decltype(tile);
@@ -769,7 +843,12 @@ void launch(const Paged& P, const AttendArgs& a, const Shape& s, hipStream_t str
     go(Tile<T, D, RW, KW, KT, WGS, true>());
   else
     go(Tile<T, D, RW, KW, KT, WGS, false>());
-  if (s.join) hipLaunchKernelGGL((join_kernel<T, D, RW * 32, SHARES>), rows, dim3(256), 0, stream, P, a);
+  if (!s.join) return;
+  const unsigned rows = (unsigned)P.T * (unsigned)a.hq;
+  if (s.parts <= 16)  // a row's: a wave takes them in a few steps
+    hipLaunchKernelGGL((join_kernel<T, D, RW * 32, SHARES, 1>), dim3((rows + 3) / 4), dim3(256), 0, stream, P, a);
+  else
+    hipLaunchKernelGGL((join_kernel<T, D, RW * 32, SHARES, 4>), dim3(rows), dim3(256), 0, stream, P, a);
 }
 
 template <typename T>
@@ -812,8 +891,8 @@ extern "C" int grid_attend(const grid_paged_cache* cache, const grid_chunks* chu
   a.q = (const uint16_t*)args->q;
   a.out = (uint16_t*)args->out;
   for (int i = 0; i < 2; ++i) {
-    a.qs[i] = args->q_stride[i];
-    a.os[i] = args->out_stride[i];
+    a.qs[i] = (uint32_t)args->q_stride[i];
+    a.os[i] = (uint32_t)args->out_stride[i];
   }
   a.lse = args->lse;
   a.runs = (int2*)args->workspace;

@@ -30,7 +30,7 @@ struct Divisor {
 
 struct Paged {
   uint16_t *k, *v;  // both dtypes have 16 bits
-  int64_t ks[3], vs[3];
+  uint32_t ks[3], vs[3];  // page, row, head
   const int32_t* table;
   int64_t table_stride;
   const int32_t* kv_len;
@@ -39,6 +39,10 @@ struct Paged {
   int32_t n_pages, cols, hkv, D, B, T;
   int64_t reach;  // positions the table has room for
 
+  // where a row of a page lies, in elements from its head's first
+  static __device__ uint64_t at(const uint32_t* stride, int page, uint32_t row) {
+    return (uint64_t)(uint32_t)page * stride[0] + (uint64_t)row * stride[1];
+  }
   // page id of position s (0 <= s < reach) of sequence b: may be out of range, see in_cache
   __device__ int page_of(int b, uint32_t s, uint32_t& row) const {
     const uint32_t c = page.quot(s);
@@ -51,7 +55,7 @@ struct Paged {
 // Checks a cache and chunks; the message names the call.
 int check_paged(const char* call, const grid_paged_cache* c, const grid_chunks* x, bool pointers);
 Paged make_paged(const grid_paged_cache* c, const grid_chunks* x);
-// Whether rows of `head_dim` at these strides (elements of 16 bits) can be read 16 bytes at a time.
+// Whether rows at these strides (elements of 16 bits, below 2^31) can be read 16 bytes at a time.
 bool rows_fit(const void* p, const int64_t* strides, int n);
 
 struct Chunk {

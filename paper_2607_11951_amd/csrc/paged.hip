@@ -6,7 +6,7 @@ namespace grid {
 bool rows_fit(const void* p, const int64_t* strides, int n) {
   if ((uintptr_t)p % 16 != 0) return false;
   for (int i = 0; i < n; ++i)
-    if (strides[i] < 0 || strides[i] % 8 != 0) return false;
+    if (strides[i] < 0 || strides[i] >= (int64_t)1 << 31 || strides[i] % 8 != 0) return false;
   return true;
 }
 
@@ -20,13 +20,14 @@ int check_paged(const char* call, const grid_paged_cache* c, const grid_chunks* 
   if (x->n_seqs < 1 || x->n_seqs > 65535) return bad("1 to 65535 sequences");
   if (x->n_tokens < 0 || x->n_tokens > 1 << 24) return bad("n_tokens");
   if (x->table_cols < 1 || x->table_stride < x->table_cols) return bad("block table");
-  if ((int64_t)x->table_cols * c->page_size > INT32_MAX) return bad("the block table has 2^31 positions or more");
+  // (positions are counted in 32 bits, a few stages past the end)
+  if ((int64_t)x->table_cols * c->page_size > INT32_MAX - 4096) return bad("the block table has 2^31 - 4096 positions or more");
   if (!pointers) return GRID_OK;
   if (!c->k_pages || !c->v_pages || !x->block_table || !x->kv_len || !x->cu_q) return bad("null pointer");
   if (!rows_fit(c->k_pages, c->k_stride, 3) || !rows_fit(c->v_pages, c->v_stride, 3))
     return bad("pages are 16-byte aligned, their strides multiples of 8");
   for (const int64_t* s : {c->k_stride, c->v_stride})
-    if (s[0] >= (int64_t)1 << 31 || s[1] >= 1 << 27 || s[2] >= 1 << 27) return bad("strides");
+    if (s[1] >= 1 << 27 || s[2] >= 1 << 27) return bad("strides");
   return GRID_OK;
 }
 
@@ -35,8 +36,8 @@ Paged make_paged(const grid_paged_cache* c, const grid_chunks* x) {
   p.k = (uint16_t*)c->k_pages;
   p.v = (uint16_t*)c->v_pages;
   for (int i = 0; i < 3; ++i) {
-    p.ks[i] = c->k_stride[i];
-    p.vs[i] = c->v_stride[i];
+    p.ks[i] = (uint32_t)c->k_stride[i];
+    p.vs[i] = (uint32_t)c->v_stride[i];
   }
   p.table = x->block_table;
   p.table_stride = x->table_stride;
