@@ -53,7 +53,7 @@ struct AttendArgs {
   int2* runs;       // [sequences][key heads]: first and last workgroup of the unit (few rows)
   Divisor group;
   int32_t hq, max_q, max_kv, window;
-  int32_t tiles, splits, len;  // many rows: tiles a sequence, ranges of len keys (a multiple of the stage)
+  int32_t blocks, tiles, splits, len;  // many rows: units of work; tiles a sequence, ranges of len keys (whole stages)
   float c;                     // |scale| * log2 e, above 0
   bool negate;                 // scale < 0: the queries are negated
 
@@ -520,11 +520,16 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void tiles_kernel(Paged P
   __shared__ int fix[3];
   no_fix(fix);
   __syncthreads();
-  uint32_t id = blockIdx.x;
+  // Runs of 16 workgroups that follow one another in the work (tiles over the same keys, most often) go to one die:
+  // workgroups are dealt to the 8 dies in turn.  Every other round of the dies is reversed, for tiles come the longest first.
+  constexpr uint32_t kRun = 16;
+  const uint32_t round = blockIdx.x / (8 * kRun), die = blockIdx.x % 8;
+  uint32_t id = (round * 8 + (round & 1 ? 7 - die : die)) * kRun + blockIdx.x / 8 % kRun;
+  if (id >= (uint32_t)a.blocks) return;
+  const int tile = a.tiles - 1 - (int)(id % (uint32_t)a.tiles);
+  id /= (uint32_t)a.tiles;
   const int split = (int)(id % (uint32_t)a.splits);
   id /= (uint32_t)a.splits;
-  const int tile = a.tiles - 1 - (int)(id % (uint32_t)a.tiles);  // the longest first
-  id /= (uint32_t)a.tiles;
   const int g = (int)(id % (uint32_t)P.hkv), b = (int)(id / (uint32_t)P.hkv);
   const Chunk ch = chunk_of(P, b);
   if (is_bad(a, ch)) {
@@ -837,7 +842,7 @@ void launch(const Paged& P, const AttendArgs& a, const Shape& s, hipStream_t str
     if constexpr (SHARES)
       hipLaunchKernelGGL((shares_kernel<T, X>), blocks, dim3(X::NT), 0, stream, P, a);
     else
-      hipLaunchKernelGGL((tiles_kernel<T, X>), blocks, dim3(X::NT), 0, stream, P, a);
+      hipLaunchKernelGGL((tiles_kernel<T, X>), dim3((blocks.x + 127) / 128 * 128), dim3(X::NT), 0, stream, P, a);
   };
   if (P.page.d % 16 == 0)
     go(Tile<T, D, RW, KW, KT, WGS, true>());
@@ -903,6 +908,7 @@ extern "C" int grid_attend(const grid_paged_cache* cache, const grid_chunks* chu
   a.max_q = args->max_q;
   a.max_kv = args->max_kv;
   a.window = args->window;
+  a.blocks = (int32_t)s.blocks;
   a.tiles = (int32_t)s.tiles;
   a.splits = s.splits;
   a.len = s.len;
