@@ -780,14 +780,20 @@ int check(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_a
 }
 
 
-// The launch.  Few rows (up to 64 a sequence and key head at most): tiles of 32 or 64 and equal shares of the stages,
-// two workgroups a compute unit, or fewer where there are fewer stages.  Many rows: tiles of 128; where they are fewer than
-// two workgroups a compute unit the keys are split, into ranges of at least 512.
+// The launch.
+//  - Up to 64 rows a sequence and key head: one tile of 32 or 64, and equal shares of the stages, two workgroups a compute
+//    unit, or fewer where there are fewer stages.
+//  - More rows: tiles of 128; where they are fewer than two workgroups a compute unit the keys are split, into ranges of
+//    at least 512.
+//  - More rows over few keys, that tiles of 32 spread over the chip at once: those.  Four waves then share a tile's keys,
+//    and nothing needs joining (7 chunks of up to 77 tokens under a window of 300, 5 key heads of 64: 8.5 us, and 14.6
+//    with tiles of 128).  Over many keys they would be read too often: 14 times for 4 chunks of 64 tokens after 8192 with
+//    7 heads a key head, that tiles of 128, split, take 61 us for.
 constexpr int kComputeUnits = 256;
 struct Shape {
   int tm, splits, len;
   int64_t tiles, blocks;
-  bool join;
+  bool shares, join;
   int64_t parts;  // of a row, at most but for one or two
   size_t slots;   // of parts
 };
@@ -798,11 +804,14 @@ Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_atten
   int64_t span = std::min<int64_t>(g->max_kv, (int64_t)x->table_cols * c->page_size);
   if (g->window) span = std::min<int64_t>(span, (int64_t)g->window + g->max_q + 127);
   const int64_t heads = (int64_t)c->n_kv_heads * x->n_seqs;
-  s.tm = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+  s.shares = rows <= 64;
+  s.tm = rows <= 32 || (rows > 64 && span <= 1024 && heads * ((rows + 31) / 32) <= 2 * kComputeUnits) ? 32
+         : rows <= 64                                                                                  ? 64
+                                                                                                       : 128;
   s.tiles = (rows + s.tm - 1) / s.tm;
   s.splits = 1;
   s.len = INT32_MAX;
-  if (s.tm < 128) {
+  if (s.shares) {
     const int64_t stage = 64, stages = (span + stage - 1) / stage;
     s.blocks = std::min<int64_t>(heads * stages, 2 * kComputeUnits);
     s.join = stages > 1;
@@ -812,7 +821,7 @@ Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_atten
   }
   s.blocks = heads * s.tiles;
   // a joining workgroup a row has to fit a launch
-  if (s.blocks < 2 * kComputeUnits && (int64_t)x->n_tokens * g->n_heads <= 1 << 22) {
+  if (s.tm == 128 && s.blocks < 2 * kComputeUnits && (int64_t)x->n_tokens * g->n_heads <= 1 << 22) {
     const int64_t len = (std::max<int64_t>(512, span * s.blocks / (4 * kComputeUnits)) + 127) / 128 * 128;
     if (len < span) {
       s.len = (int)len;
@@ -833,16 +842,14 @@ size_t workspace_of(const grid_paged_cache* c, const grid_chunks* x, const Shape
   return runs_bytes(c, x) + s.slots * (size_t)s.tm * (size_t)(c->head_dim + 2) * 4;
 }
 
-template <typename T, int D, int RW, int KW, int KT, int WGS>
+template <typename T, int D, int RW, int KW, int KT, int WGS, bool SHARES>
 void launch(const Paged& P, const AttendArgs& a, const Shape& s, hipStream_t stream) {
-  const dim3 blocks((unsigned)s.blocks);
-  constexpr bool SHARES = RW * 32 < 128;
   const auto go = [&](auto tile) {
     using X = decltype(tile);
     if constexpr (SHARES)
-      hipLaunchKernelGGL((shares_kernel<T, X>), blocks, dim3(X::NT), 0, stream, P, a);
+      hipLaunchKernelGGL((shares_kernel<T, X>), dim3((unsigned)s.blocks), dim3(X::NT), 0, stream, P, a);
     else
-      hipLaunchKernelGGL((tiles_kernel<T, X>), dim3((blocks.x + 127) / 128 * 128), dim3(X::NT), 0, stream, P, a);
+      hipLaunchKernelGGL((tiles_kernel<T, X>), dim3((unsigned)((s.blocks + 127) / 128 * 128)), dim3(X::NT), 0, stream, P, a);
   };
   if (P.page.d % 16 == 0)
     go(Tile<T, D, RW, KW, KT, WGS, true>());
@@ -856,20 +863,33 @@ void launch(const Paged& P, const AttendArgs& a, const Shape& s, hipStream_t str
     hipLaunchKernelGGL((join_kernel<T, D, RW * 32, SHARES, 4>), dim3(rows), dim3(256), 0, stream, P, a);
 }
 
+// Waves of rows and of keys, keys a wave and workgroups a compute unit, by what fits in LDS and registers.
 template <typename T>
 void choose(const Paged& P, const AttendArgs& a, const Shape& s, hipStream_t stream) {
+  const auto with = [&](auto few, auto some, auto many, auto narrow) {
+    if (s.tm == 128)
+      many();
+    else if (!s.shares)
+      narrow();
+    else if (s.tm == 32)
+      few();
+    else
+      some();
+  };
   if (P.D == 64)
-    s.tm == 32   ? launch<T, 64, 1, 4, 32, 2>(P, a, s, stream)
-    : s.tm == 64 ? launch<T, 64, 2, 2, 32, 2>(P, a, s, stream)
-                 : launch<T, 64, 4, 1, 64, 2>(P, a, s, stream);
+    with([&] { launch<T, 64, 1, 4, 32, 2, true>(P, a, s, stream); }, [&] { launch<T, 64, 2, 2, 32, 2, true>(P, a, s, stream); },
+         [&] { launch<T, 64, 4, 1, 128, 2, false>(P, a, s, stream); },
+         [&] { launch<T, 64, 1, 4, 32, 2, false>(P, a, s, stream); });
   else if (P.D == 128)
-    s.tm == 32   ? launch<T, 128, 1, 4, 32, 2>(P, a, s, stream)
-    : s.tm == 64 ? launch<T, 128, 2, 2, 32, 2>(P, a, s, stream)
-                 : launch<T, 128, 4, 1, 64, 2>(P, a, s, stream);
+    with([&] { launch<T, 128, 1, 4, 32, 2, true>(P, a, s, stream); },
+         [&] { launch<T, 128, 2, 2, 32, 2, true>(P, a, s, stream); },
+         [&] { launch<T, 128, 4, 1, 64, 2, false>(P, a, s, stream); },
+         [&] { launch<T, 128, 1, 4, 32, 2, false>(P, a, s, stream); });
   else
-    s.tm == 32   ? launch<T, 256, 1, 4, 32, 1>(P, a, s, stream)
-    : s.tm == 64 ? launch<T, 256, 2, 2, 32, 1>(P, a, s, stream)
-                 : launch<T, 256, 4, 1, 32, 1>(P, a, s, stream);
+    with([&] { launch<T, 256, 1, 4, 32, 1, true>(P, a, s, stream); },
+         [&] { launch<T, 256, 2, 2, 32, 1, true>(P, a, s, stream); },
+         [&] { launch<T, 256, 4, 1, 32, 1, false>(P, a, s, stream); },
+         [&] { launch<T, 256, 1, 4, 32, 1, false>(P, a, s, stream); });
 }
 
 }  // namespace
