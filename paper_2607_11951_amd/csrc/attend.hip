@@ -53,7 +53,8 @@ struct AttendArgs {
   int2* runs;       // [sequences][key heads]: first and last workgroup of the unit (few rows)
   Divisor group;
   int32_t hq, max_q, max_kv, window;
-  int32_t blocks, tiles, splits, len;  // many rows: units of work; tiles a sequence, ranges of len keys (whole stages)
+  // many rows: workgroups; tiles a sequence and key head, ranges of len keys (whole stages); units side by side
+  int32_t blocks, tiles, splits, len, bundle;
   float c;                     // |scale| * log2 e, above 0
   bool negate;                 // scale < 0: the queries are negated
 
@@ -157,7 +158,8 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
   const int pos_max = first_pos + (int)a.group.quot((uint32_t)min(r0 + 31, rows - 1));
 
   // Loads.  Load i of a wave brings RPI rows from row WR * wave + i * RPI of the stage on, a lane piece `lane % PR` of
-  // row `lane / PR`; rows at and after s_hi are the last row again.
+  // row `lane / PR`.  At and after s_hi come rows that the same page holds, or the last ones again: nothing
+  // is made of them, whatever they hold.
   const uint32_t base = (uint32_t)(uintptr_t)(GRID_LDS uint8_t*)lds;
   const uint16_t *kg = P.k + (uint64_t)g * P.ks[2], *vg = P.v + (uint64_t)g * P.vs[2];
   const auto* table = (const __attribute__((address_space(4))) int32_t*)(P.table + (int64_t)b * P.table_stride);
@@ -182,7 +184,7 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
       page[i] = in ? page[i] : 0;
     }
   };
-  const auto fetch = [&](const uint16_t* x, const uint32_t* st, int s0, uint32_t to) {
+  const auto fetch = [&](const uint16_t* x, const uint32_t* st, uint32_t to) {
     to += (uint32_t)(wave * WR * D * 2);
     const uint32_t step = lrow * st[1];
 #pragma unroll
@@ -190,14 +192,10 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
       const int piece = lane % PR ^ swz<D>(wave * WR + i * RPI + lrow);
       if constexpr (UNI) {
         constexpr int PER = RUN / RPI;
-        const int f = i / PER, s = s0 + wave * WR + f * RUN, before = i % PER * RPI;
         // (scalars, whatever registers they were kept in)
-        const int pg = __builtin_amdgcn_readfirstlane(page[f]);
-        const uint32_t r = (uint32_t)__builtin_amdgcn_readfirstlane((int)row[f]);
-        const int last = s_hi - 1 - min(s, (s_hi - 1) & ~(RUN - 1));  // last row of the run to read
-        const uint16_t* p = x + P.at(st, pg, r + (uint32_t)min(before, last));
-        const uint32_t lr = last >= RUN - 1 ? step : (uint32_t)min(lrow, max(last - before, 0)) * st[1];
-        to_lds(p, (lr + piece * 8) * 2, to + i * 1024);
+        const int pg = __builtin_amdgcn_readfirstlane(page[i / PER]);
+        const uint32_t r = (uint32_t)__builtin_amdgcn_readfirstlane((int)row[i / PER]);
+        to_lds(x + P.at(st, pg, r + (uint32_t)(i % PER * RPI)), (step + piece * 8) * 2, to + i * 1024);
       } else {
         to_lds(x + P.at(st, page[i], row[i]) + piece * 8, to + i * 1024);
       }
@@ -226,25 +224,33 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
   // S^T of the wave's keys
   float16_v s[KB];
   const auto scores = [&](const uint8_t* ks) {
+    // Piece 2 k + half of the row, at its place: the bits of k by exclusive or, which is one instruction with the sum.
+    int at = col * D * 2 + (half ^ swz<D>(col)) * 16;
+    asm volatile("" : "+v"(at));  // anew every time: registers are short
+    constexpr int N = QS * KB, AHEAD = 6;
+    Eight kk[N];
+    const auto read = [&](int j) { kk[j] = *(const Eight*)(ks + (at ^ j / KB * 32) + j % KB * 32 * D * 2); };
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
+    for (int j = 0; j < AHEAD && j < N; ++j) read(j);
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[kb][i] = 0.f;
 #pragma unroll
-      for (int k = 0; k < QS; ++k) {
-        const int piece = (2 * k + half) ^ swz<D>(col);
-        const Eight kk = *(const Eight*)(ks + (kb * 32 + col) * D * 2 + piece * 16);
-        s[kb] = Vec<T>::mfma(kk, q[k], s[kb]);
-      }
+    for (int j = 0; j < N; ++j) {
+      if (j + AHEAD < N) read(j + AHEAD);
+      s[j % KB] = Vec<T>::mfma(kk[j], q[j / KB], s[j % KB]);
+      if constexpr (!PRIV) __builtin_amdgcn_sched_barrier(0);
     }
   };
   const auto mask = [&](int k0) {
-    const int hi = min(pos, s_hi - 1), lo = a.window ? pos - a.window : -1;
+    // the lane's keys are k0 + 4 * half and constants more
+    const int from = k0 + 4 * half, hi = min(pos, s_hi - 1) - from, lo = (a.window ? pos - a.window : -1) - from;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int key = k0 + kb * 32 + 8 * (i / 4) + 4 * half + i % 4;
+        const int key = kb * 32 + 8 * (i / 4) + i % 4;
         s[kb][i] = key <= hi && key > lo ? s[kb][i] : -INFINITY;
       }
   };
@@ -305,6 +311,11 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
       }
   };
   const auto sums = [&](const uint8_t* vs) {
+    // V's operand: entry d * 32 + col of 8 keys, in the order the scores lie in.  A lane reads of rows
+    // 16 t + 8 j + rr the pieces 4 d + piece, at their places.
+    const int l16 = lane & 15, rr = 4 * half + (l16 >> 2), piece = (lane >> 4 & 1) * 2 + (l16 >> 1 & 1);
+    int at = rr * D * 2 + (piece ^ swz<D>(rr)) * 16 + (l16 & 1) * 8;
+    asm volatile("" : "+v"(at));
 #pragma unroll
     for (int t = 0; t < KT / 16; ++t) {
       Eight p;
@@ -312,18 +323,14 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
       for (int i = 0; i < 8; ++i) p[i] = (T)s[t / 2][t % 2 * 8 + i];
 #pragma unroll
       for (int d = 0; d < DB; ++d) {
-        // V's operand: entry d * 32 + col of 8 keys, in the order the scores lie in
         union {
           short4_v four[2];
           Eight all;
         } v;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int l16 = lane & 15, rr = 16 * t + 8 * j + 4 * half + (l16 >> 2);
-          const int piece = (d * 4 + (lane >> 4 & 1) * 2 + (l16 >> 1 & 1)) ^ swz<D>(rr);
+        for (int j = 0; j < 2; ++j)  // (the swizzle of a row 8 on differs by 2)
           v.four[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (GRID_LDS short4_v*)(vs + rr * D * 2 + piece * 16 + (l16 & 1) * 8));
-        }
+              (GRID_LDS short4_v*)(vs + (at ^ (d * 4 ^ j * 2) * 16) + (16 * t + 8 * j) * D * 2));
         o[d] = Vec<T>::mfma(v.all, p, o[d]);
       }
     }
@@ -333,8 +340,8 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
     const uint8_t *ks = lds + kw * KT * D * 2, *vs = ks + kHalf;
     if (s_lo + kw * KT < s_hi) {
       find(s_lo);
-      fetch(kg, P.ks, s_lo, base);
-      fetch(vg, P.vs, s_lo, base + kHalf);
+      fetch(kg, P.ks, base);
+      fetch(vg, P.vs, base + kHalf);
       load_q();
     }
     for (int s0 = s_lo; s0 + kw * KT < s_hi; s0 += SK) {
@@ -345,7 +352,7 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
       scores(ks);
       wait_reads();
       if (more) {
-        fetch(kg, P.ks, s0 + SK, base);
+        fetch(kg, P.ks, base);
         wait_loads<LOADS>();
       } else {
         wait_loads<0>();
@@ -357,12 +364,12 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
       softmax();
       sums(vs);
       wait_reads();
-      if (more) fetch(vg, P.vs, s0 + SK, base + kHalf);
+      if (more) fetch(vg, P.vs, base + kHalf);
     }
   } else {
     find(s_lo);
-    fetch(kg, P.ks, s_lo, base);
-    fetch(vg, P.vs, s_lo, base + kHalf);
+    fetch(kg, P.ks, base);
+    fetch(vg, P.vs, base + kHalf);
     load_q();
     if (s_lo + SK < s_hi) find(s_lo + SK);
     // stages that some row of the tile does not see all of
@@ -377,8 +384,8 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
     uint32_t buf = 0;
     for (int s0 = s_lo; s0 < s_hi; s0 += SK) {
       if (s0 + SK < s_hi) {
-        fetch(kg, P.ks, s0 + SK, base + (buf ^ 2 * kHalf));
-        fetch(vg, P.vs, s0 + SK, base + (buf ^ 2 * kHalf) + kHalf);
+        fetch(kg, P.ks, base + (buf ^ 2 * kHalf));
+        fetch(vg, P.vs, base + (buf ^ 2 * kHalf) + kHalf);
         if (s0 + 2 * SK < s_hi) find(s0 + 2 * SK);
       }
       const int k0 = s0 + kw * KT;
@@ -520,16 +527,31 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void tiles_kernel(Paged P
   __shared__ int fix[3];
   no_fix(fix);
   __syncthreads();
-  // Runs of 16 workgroups that follow one another in the work (tiles over the same keys, most often) go to one die:
-  // workgroups are dealt to the 8 dies in turn.  Every other round of the dies is reversed, for tiles come the longest first.
-  constexpr uint32_t kRun = 16;
-  const uint32_t round = blockIdx.x / (8 * kRun), die = blockIdx.x % 8;
-  uint32_t id = (round * 8 + (round & 1 ? 7 - die : die)) * kRun + blockIdx.x / 8 % kRun;
-  if (id >= (uint32_t)a.blocks) return;
-  const int tile = a.tiles - 1 - (int)(id % (uint32_t)a.tiles);
-  id /= (uint32_t)a.tiles;
-  const int split = (int)(id % (uint32_t)a.splits);
-  id /= (uint32_t)a.splits;
+  // Workgroups are dealt to the 8 dies in turn; a die is to read the same keys for the tiles that it runs together.  A unit
+  // is a sequence and key head.
+  const uint32_t per = (uint32_t)(a.tiles * a.splits);
+  uint32_t id, rank;
+  if (a.bundle == 0) {
+    // Many units that all run at once: runs of 16 that follow one another go to one die, so that the keys are shared and chunks of many
+    // tiles spread over the dies; every other round of the dies is reversed, for a unit's tiles come the longest first (7 chunks of up to 77 tokens, a window of 300, 5 key heads: 8.2 us; with a unit a die 9.2,
+    // with an eighth of them all a die 9.9).
+    constexpr uint32_t kRun = 16;
+    const uint32_t round = blockIdx.x / (8 * kRun), die = blockIdx.x % 8;
+    const uint32_t at = (round * 8 + (round & 1 ? 7 - die : die)) * kRun + blockIdx.x / 8 % kRun;
+    if (at >= (uint32_t)a.blocks) return;
+    id = at / per;
+    rank = at - id * per;
+  } else {
+    // `bundle` units side by side, the longest tiles of all first, so that the last to run are short (of ranges of keys the
+    // last ones, that early rows see little of).  A die has its own units of a bundle of a multiple of 8, or of 4 or 2
+    // shares them with few others.  (A chunk of 2048 tokens after 4096, 4 units of 112 tiles: 175 us, in runs of 16 213.)
+    const uint32_t begun = blockIdx.x / ((uint32_t)a.bundle * per), in = blockIdx.x - begun * (uint32_t)a.bundle * per;
+    if (blockIdx.x >= (uint32_t)a.blocks) return;
+    const uint32_t first = begun * (uint32_t)a.bundle, side = min((uint32_t)a.bundle, (uint32_t)a.blocks / per - first);
+    rank = in / side;
+    id = first + in - rank * side;
+  }
+  const int split = (int)(rank / (uint32_t)a.tiles), tile = a.tiles - 1 - (int)(rank % (uint32_t)a.tiles);
   const int g = (int)(id % (uint32_t)P.hkv), b = (int)(id / (uint32_t)P.hkv);
   const Chunk ch = chunk_of(P, b);
   if (is_bad(a, ch)) {
@@ -783,8 +805,9 @@ int check(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_a
 // The launch.
 //  - Up to 64 rows a sequence and key head: one tile of 32 or 64, and equal shares of the stages, two workgroups a compute
 //    unit, or fewer where there are fewer stages.
-//  - More rows: tiles of 128; where they are fewer than two workgroups a compute unit the keys are split, into ranges of
-//    at least 512.
+//  - More rows: tiles of 128; where they are fewer than 3/4 of the workgroups that run at once the keys are split, into
+//    ranges of at least 512 (a chunk after a cache, 6144 keys together, 28 heads on 4 of 128: of 1280 tokens 148 us split
+//    and 160 whole, of 2048, 7/8 of the workgroups, 202 and 175).
 //  - More rows over few keys, that tiles of 32 spread over the chip at once: those.  Four waves then share a tile's keys,
 //    and nothing needs joining (7 chunks of up to 77 tokens under a window of 300, 5 key heads of 64: 8.5 us, and 14.6
 //    with tiles of 128).  Over many keys they would be read too often: 14 times for 4 chunks of 64 tokens after 8192 with
@@ -794,6 +817,7 @@ struct Shape {
   int tm, splits, len;
   int64_t tiles, blocks;
   bool shares, join;
+  int64_t at_once;  // workgroups that run side by side (many rows)
   int64_t parts;  // of a row, at most but for one or two
   size_t slots;   // of parts
 };
@@ -811,6 +835,7 @@ Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_atten
   s.tiles = (rows + s.tm - 1) / s.tm;
   s.splits = 1;
   s.len = INT32_MAX;
+  s.at_once = (c->head_dim == 256 ? 1 : 2) * kComputeUnits;
   if (s.shares) {
     const int64_t stage = 64, stages = (span + stage - 1) / stage;
     s.blocks = std::min<int64_t>(heads * stages, 2 * kComputeUnits);
@@ -821,11 +846,11 @@ Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_atten
   }
   s.blocks = heads * s.tiles;
   // a joining workgroup a row has to fit a launch
-  if (s.tm == 128 && s.blocks < 2 * kComputeUnits && (int64_t)x->n_tokens * g->n_heads <= 1 << 22) {
+  if (s.tm == 128 && 4 * s.blocks < 3 * s.at_once && (int64_t)x->n_tokens * g->n_heads <= 1 << 22) {
     const int64_t len = (std::max<int64_t>(512, span * s.blocks / (4 * kComputeUnits)) + 127) / 128 * 128;
-    if (len < span) {
-      s.len = (int)len;
+    if (len < span) {  // ranges alike
       s.splits = (int)((span + len - 1) / len);
+      s.len = (int)(((span + s.splits - 1) / s.splits + 127) / 128 * 128);
       s.blocks *= s.splits;
     }
   }
@@ -932,6 +957,9 @@ extern "C" int grid_attend(const grid_paged_cache* cache, const grid_chunks* chu
   a.tiles = (int32_t)s.tiles;
   a.splits = s.splits;
   a.len = s.len;
+  // as many units side by side as fill the chip
+  const int64_t per = s.tiles * s.splits, units = s.blocks / per, fill = (s.at_once + per - 1) / per;
+  a.bundle = s.blocks <= s.at_once && units > 8 ? 0 : (int32_t)std::min<int64_t>(units, (fill + 7) / 8 * 8);
   a.negate = args->scale < 0.f;
   a.c = std::fmin(std::fmax(std::fabs(args->scale) * kLog2e, 1e-30f), 1e30f);
   const Paged P = make_paged(cache, chunks);
