@@ -3,6 +3,9 @@
 // A head's vector of one token is 8 entries (16 bytes) a lane, so a power of two of lanes holds one; its mean square is
 // their sum across those lanes.  Both entries of a rotated pair are needed at once: side by side they are in one lane;
 // half a rotation apart the partner's 16 bytes are exchanged between the lanes.
+//
+// Bound by bytes, for few tokens by dependent reads: 8 chunks of up to 2048 tokens, 32 + 8 + 8 heads of 128 in float16,
+// half of each rotated, take 55.5 us, 4.5 TB/s (a copy reaches 5.09); one token 3.2 us on the device.
 #include "lanes.h"
 #include "paged.h"
 

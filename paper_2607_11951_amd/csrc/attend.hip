@@ -9,6 +9,14 @@
 // its row's maximum and sum are the lane's own but for one exchange between the wave's halves, and its weights, rounded
 // and packed, are in place as the second operand of O^T += V^T P^T: that product adds over keys in any order, so V's
 // rows are read, transposed on the way from LDS, in the order the scores lie in.
+//
+// Bounds (bf16, heads of 128; a copy reaches 5.09 TB/s here, a product of 8192^3 1392 TFLOP/s).  Few rows read the cache
+// once: 64 sequences of up to 8192 keys, 8 key heads, one token each, take 181 us, 4.97 TB/s of it; 32 of up to 4096, 4 key
+// heads, up to 5 tokens, 44 us, 3.1 TB/s (34 the shares, 8 stages each, 5 the joining); one of 1500 keys 11 us, two launches
+// of dependent reads.  Prompts are bound by the vector and matrix units together, which hardly overlap here (43 % and 42 %
+// busy): 2 chunks of 2048 tokens after 4096, 28 heads on 4, take 320 us, 940 TFLOP/s, batches of 16 of them 1027.  So the
+// weights' exponentials, sums and roundings are nearly all that is left of the vector instructions in a stage, and
+// scores a stage ahead of the sums, their instructions woven into the weights', are slower for the registers they need.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -533,8 +541,9 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void tiles_kernel(Paged P
   uint32_t id, rank;
   if (a.bundle == 0) {
     // Many units that all run at once: runs of 16 that follow one another go to one die, so that the keys are shared and chunks of many
-    // tiles spread over the dies; every other round of the dies is reversed, for a unit's tiles come the longest first (7 chunks of up to 77 tokens, a window of 300, 5 key heads: 8.2 us; with a unit a die 9.2,
-    // with an eighth of them all a die 9.9).
+    // tiles spread over the dies; every other round of the dies is reversed, for a unit's tiles come the longest first
+    // (7 chunks of up to 77 tokens, a window of 300, 5 key heads: 8.2 us; with a unit a die 9.2, with an eighth of them all
+    // a die 9.9).
     constexpr uint32_t kRun = 16;
     const uint32_t round = blockIdx.x / (8 * kRun), die = blockIdx.x % 8;
     const uint32_t at = (round * 8 + (round & 1 ? 7 - die : die)) * kRun + blockIdx.x / 8 % kRun;
