@@ -961,7 +961,9 @@ extern "C" int grid_attend(const grid_paged_cache* cache, const grid_chunks* chu
   a.hq = args->n_heads;
   a.max_q = args->max_q;
   a.max_kv = args->max_kv;
-  a.window = args->window;
+  // A window that no position exceeds is none, so positions less it and a few stages stay in 32 bits.
+  const int64_t most = std::min<int64_t>(args->max_kv, (int64_t)chunks->table_cols * cache->page_size);
+  a.window = args->window >= most ? 0 : args->window;
   a.blocks = (int32_t)s.blocks;
   a.tiles = (int32_t)s.tiles;
   a.splits = s.splits;

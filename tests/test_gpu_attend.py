@@ -162,6 +162,17 @@ def test_long_caches(G, lens, dtype):
     agree(bt.attend(G, window=9000), bt, window=9000)
 
 
+@pytest.mark.parametrize("window", [1025, 4097, 1 << 30, (1 << 31) - 1])
+def test_windows_that_hide_nothing(G, window):
+    """as long as the longest sequence or longer, up to the largest there is: the same bits as without"""
+    for heads in ((28, 4, 128), (4, 4, 64), (2, 1, 256)):
+        bt = Batch(MIXED, heads, 16, "bf16", seed=3)
+        want, got = bt.attend(G), bt.attend(G, window=window)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        got = bt.attend(G, window=window, max_kv=(1 << 31) - 1)
+        agree(got, bt)
+
+
 def test_many_sequences(G):
     lens = [(i % 4, 3 + 7 * i % 400) for i in range(300)]
     bt = Batch(lens, (8, 2, 64), 16, "bf16", seed=6)
