@@ -817,10 +817,14 @@ int check(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_a
 //  - More rows: tiles of 128; where they are fewer than 3/4 of the workgroups that run at once the keys are split, into
 //    ranges of at least 512 (a chunk after a cache, 6144 keys together, 28 heads on 4 of 128: of 1280 tokens 148 us split
 //    and 160 whole, of 2048, 7/8 of the workgroups, 202 and 175).
-//  - More rows over few keys, that tiles of 32 spread over the chip at once: those.  Four waves then share a tile's keys,
-//    and nothing needs joining (7 chunks of up to 77 tokens under a window of 300, 5 key heads of 64: 8.5 us, and 14.6
-//    with tiles of 128).  Over many keys they would be read too often: 14 times for 4 chunks of 64 tokens after 8192 with
-//    7 heads a key head, that tiles of 128, split, take 61 us for.
+//  - Few keys, where tiles of 32 run all at once: those, a workgroup each for all its keys.  Four waves share a tile's
+//    keys, and nothing needs joining.  Up to 64 rows that saves the joining launch and costs the keys in turn: a token of 28
+//    heads on 4 of 128 after 256 keys takes 7.0 us so and 10.2 shared, after 512 9.4 and 10.6, after 1024 14.6 and 10.4;
+//    where the tiles fill the chip shares only add parts (64 tokens, 32 heads on 8, 1 to 2048 keys: 48 us and 59; 32
+//    chunks of 8: 30 and 42).  Heads of 256 have one workgroup a compute unit, and are slower so sooner.  Of more rows: 7
+//    chunks of up to 77 tokens under a window of 300, 5 key heads of 64, 8.5 us, and 14.6 with tiles of 128.  Over many
+//    keys they would be read too often: 14 times for 4 chunks of 64 tokens after 8192 with 7 heads a key head, that tiles of
+//    128, split, take 61 us for.
 constexpr int kComputeUnits = 256;
 struct Shape {
   int tm, splits, len;
@@ -837,8 +841,15 @@ Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_atten
   int64_t span = std::min<int64_t>(g->max_kv, (int64_t)x->table_cols * c->page_size);
   if (g->window) span = std::min<int64_t>(span, (int64_t)g->window + g->max_q + 127);
   const int64_t heads = (int64_t)c->n_kv_heads * x->n_seqs;
-  s.shares = rows <= 64;
-  s.tm = rows <= 32 || (rows > 64 && span <= 1024 && heads * ((rows + 31) / 32) <= 2 * kComputeUnits) ? 32
+  const int64_t small = heads * ((rows + 31) / 32);  // tiles of 32
+  const int few_keys = rows > 64                   ? 1024
+                       : c->head_dim == 256        ? 384
+                       : small >= kComputeUnits     ? 2048
+                       : small >= kComputeUnits / 2 ? 1024
+                                                    : 640;
+  const bool narrow = small <= 2 * kComputeUnits && span <= few_keys;
+  s.shares = rows <= 64 && !narrow;
+  s.tm = rows <= 32 || narrow ? 32
          : rows <= 64                                                                                  ? 64
                                                                                                        : 128;
   s.tiles = (rows + s.tm - 1) / s.tm;

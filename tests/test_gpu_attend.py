@@ -286,6 +286,65 @@ def test_bad_sequences_are_nan(G):
     check(bt, [4])
 
 
+WIDE = {"extra_cols": 130}  # bounds of 2000 positions: the launches of long caches, whatever the lengths
+
+
+@pytest.mark.parametrize("poison", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("heads", [(8, 2, 128), (4, 4, 64), (4, 1, 256)])
+@pytest.mark.parametrize("lens", [[(5, 130), (1, 31), (0, 7)], [(12, 90), (3, 3), (1, 700)]])
+def test_what_is_not_seen_has_no_part_under_long_bounds(G, poison, heads, lens):
+    window = 40
+    bt = Batch(lens, heads, 16, "bf16", seed=21, spare=3, **WIDE)
+    clean = bt.attend(G, window=window, max_kv=2000)
+    agree(clean, bt, window=window)
+    for pages in (bt.k, bt.v):
+        pages[torch.from_numpy(bt.free.astype(np.int64)).cuda()] = poison
+        for b, (n, kv) in enumerate(lens):
+            if kv % bt.page:
+                pages[int(bt.table_host[b, kv // bt.page]), kv % bt.page:] = poison
+            hidden = np.arange(max(0, kv - n - window + 1))
+            page, row = bt.rows(b, hidden)
+            pages[torch.from_numpy(page.astype(np.int64)).cuda(), torch.from_numpy(row).cuda()] = poison
+    got = bt.attend(G, window=window, max_kv=2000)
+    assert torch.equal(got[0], clean[0]) and torch.equal(got[1], clean[1])
+
+
+@pytest.mark.parametrize("lens", [[(2, 90), (1, 40), (3, 64), (1, 100)], [(2, 90), (1, 40), (3, 64), (14, 900)]])
+def test_bad_sequences_are_nan_under_long_bounds(G, lens):
+    def fresh():
+        return Batch(lens, (8, 2, 128), 16, "bf16", seed=22, **WIDE)
+
+    good = fresh()
+
+    def check(bt, bad, **kw):
+        got = bt.attend(G, **{"max_kv": 2000, **kw})
+        rows = torch.zeros(bt.T, dtype=torch.bool, device="cuda")
+        rows[int(bt.cu_host[bad]):int(bt.cu_host[bad + 1])] = True
+        agree(got, good, rows=~rows)
+        assert bool(torch.isnan(got[0][rows].float()).all()) and bool(torch.isnan(got[1][rows]).all())
+
+    bt = fresh()
+    bt.table[0, 1] = bt.P
+    check(bt, 0)
+    bt = fresh()
+    bt.kv_len[1] = 1 << 30
+    check(bt, 1)
+    bt = fresh()
+    bt.kv_len[2] = 2
+    check(bt, 2)
+    bt = fresh()
+    bt.cu[4] = 10000  # the last chunk reaches past the packed rows
+    check(bt, 3)
+
+
+@pytest.mark.parametrize("kv", [640, 641, 1024, 1025, 2048, 2049])
+def test_lengths_around_the_launches(G, kv):
+    for B, heads in ((1, (28, 4, 128)), (33, (16, 4, 64)), (70, (8, 4, 128)), (1, (8, 1, 256))):
+        lens = [(1 + i % 3, max(3, kv - 29 * i)) for i in range(B)]
+        bt = Batch(lens, heads, 32, "bf16", seed=kv)
+        agree(bt.attend(G), bt)
+
+
 def test_rows_of_no_sequence_are_left(G):
     bt = Batch([(3, 20), (2, 70)], (4, 2, 64), 16, "bf16", seed=14)
     bt.q = bt.rand((bt.T + 6, bt.hq, bt.D))
