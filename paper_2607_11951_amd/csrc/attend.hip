@@ -88,12 +88,18 @@ __device__ inline float other_half(float x) {  // the value of lane ^ 32
 // 16 bytes a lane from global memory (uniform base + the lane's offset in bytes) to LDS at `to` + 16 * lane (to:
 // uniform, bytes from the start of LDS).  Written as assembly because the compiler waits for all such loads before any
 // LDS read; they are counted by vmcnt.  LDS reads issued before are waited for first: they may be of what is overwritten.
+// The compiler counts no wait states in here: a load into LDS needs one after the write of M0.
+// (M0 is among the registers that the compiler allots to nothing, which it remarks on.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ inline void to_lds(const void* base, uint32_t offset, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to) : "memory");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to)
+               : "memory", "m0");
 }
 __device__ inline void to_lds(const void* from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 template <int N>  // until at most the last N are under way
 __device__ inline void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
