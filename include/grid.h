@@ -590,10 +590,12 @@ typedef struct {
  * with the chunk.  Position s of sequence b is row s % page_size of page
  * block_table[b * table_stride + s / page_size].  A chunk may be empty; tokens
  * before cu_q[0] and from cu_q[n_seqs] on belong to no sequence.  A sequence
- * is bad when cu_q[b] < 0, cu_q[b + 1] < cu_q[b], cu_q[b + 1] > n_tokens,
- * or kv_len[b] is less than the chunk or more than table_cols * page_size; what
- * a call does with it, and with a page id that is not in 0 .. n_pages - 1, is
- * said there.  No call leaves the cache's bounds. */
+ * is bad when kv_len[b] is less than the chunk or more than table_cols *
+ * page_size.  When cu_q[b] < 0, cu_q[b + 1] < cu_q[b] or cu_q[b + 1] >
+ * n_tokens, sequence b and all after it are bad, and the tokens from cu_q[b] to
+ * the last are theirs.  What a call does with a bad sequence, and with a page id
+ * that is not in 0 .. n_pages - 1, is said there.  No call leaves the cache's
+ * bounds. */
 typedef struct {
   int32_t n_seqs;              /* B, 1 .. 65535 */
   int32_t n_tokens;            /* rows of the packed arrays, 0 .. 2^24 */

@@ -31,10 +31,11 @@ struct alignas(16) Eight {
   T x[8];
 };
 
-// A sequence's status: whether every one of its chunk's tokens has a place and a rotation.
-__device__ int status_of(const Paged& P, const AppendArgs& a, int b) {
+// The status of a sequence after chunks that are in order or not: whether every one of its chunk's tokens has a place
+// and a rotation.
+__device__ int status_of(const Paged& P, const AppendArgs& a, int b, bool ordered) {
   const Chunk c = chunk_of(P, b);
-  bool ok = c.ok && (!a.cos || c.kv <= a.n_positions || c.n == 0);
+  bool ok = ordered && c.ok && (!a.cos || c.kv <= a.n_positions || c.n == 0);
   if (ok && c.n > 0) {
     const uint32_t from = P.page.quot((uint32_t)(c.kv - c.n)), to = P.page.quot((uint32_t)(c.kv - 1));
     for (uint32_t p = from; p <= to; ++p) ok = ok && P.in_cache(P.table[(int64_t)b * P.table_stride + p]);
@@ -46,14 +47,23 @@ enum class Turn { kNone, kHalves, kPairs };
 
 // One workgroup a token; the workgroups after the last token write the statuses.  What a token needs hangs on reads one
 // after the other (its sequence and lengths, its page, its cosines), so the vectors, which hang on nothing, are asked for
-// first, and the sequence's lengths with its search: the lanes hold those of 64 sequences, and the one that is found hands
-// its own out.  A lane takes the same entries of all its vectors: the cosines are read once.
+// first, and the sequence's lengths with its search.  A lane takes the same entries of all its vectors: the cosines are
+// read once.
 template <typename T, Turn TURN, bool NORM>
 __global__ __launch_bounds__(kThreads) void append_kernel(Paged P, AppendArgs a) {
   const int t = (int)blockIdx.x, tid = (int)threadIdx.x, lane = tid & 63;
   if (t >= P.T) {
     const int b = (t - P.T) * kThreads + tid;
-    if (b < P.B) a.status[b] = status_of(P, a, b);
+    __shared__ int broken;  // the first of the sequences up to here whose chunk is not in order
+    if (tid == 0) broken = P.B;
+    __syncthreads();
+    for (int s = tid; s < min(b - tid + kThreads, P.B); s += kThreads)
+      if (!in_order(P, P.cu_q[s], P.cu_q[s + 1])) {
+        atomicMin(&broken, s);
+        break;
+      }
+    __syncthreads();
+    if (b < P.B) a.status[b] = status_of(P, a, b, b <= broken);
     return;
   }
   const int part = tid & (a.lanes - 1), groups = kThreads / a.lanes, e = part * 8;  // e: the lane's first entry
@@ -75,21 +85,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Paged P, AppendArgs a)
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i)
     if (u_first + i * groups < vectors) ahead[i] = source(u_first + i * groups);
-  // the token's sequence: as many as end at or before it
-  Chunk c;
-  c.ok = false;
-  int b = 0;
-  for (int s = 0; s < P.B; s += 64) {
-    const int x = min(s + lane, P.B - 1);
-    const int32_t first = P.cu_q[x], end = P.cu_q[x + 1], kv = P.kv_len[x];
-    const int before = __popcll(__ballot(s + lane < P.B && end <= t));
-    b += before;
-    if (before < min(64, P.B - s)) {
-      c = chunk_of(P, __builtin_amdgcn_readlane(first, before), __builtin_amdgcn_readlane(end, before),
-                   __builtin_amdgcn_readlane(kv, before));
-      break;
-    }
-  }
+  int b;
+  const Chunk c = chunk_of_token(P, t, b);
   if (!c.ok || t < c.first || t >= c.first + c.n) return;
   const int pos = c.kv - c.n + t - c.first;
   if (TURN != Turn::kNone && pos >= a.n_positions) return;

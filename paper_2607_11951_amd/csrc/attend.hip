@@ -21,6 +21,7 @@
 #include <cmath>
 #include <type_traits>
 
+#include "lanes.h"
 #include "paged.h"
 
 using namespace grid;
@@ -523,10 +524,11 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
   }
 }
 
-// The rows of a bad sequence.
+// The rows of a bad sequence, of the first whose chunk is not in order all that follow: those after it are bad too.
 template <typename T, int D>
 __device__ void fill_nan(const Paged& P, const AttendArgs& a, const Chunk& ch, int b, int nt) {
-  const int from = min(max(ch.first, 0), P.T), to = min(max(P.cu_q[b + 1], from), P.T);
+  const int32_t end = P.cu_q[b + 1];
+  const int from = min(max(ch.first, 0), P.T), to = in_order(P, ch.first, end) ? end : P.T;
   for (int64_t i = threadIdx.x; i < (int64_t)(to - from) * a.hq * D; i += nt) {
     const int t = from + (int)(i / (a.hq * D)), e = (int)(i % (a.hq * D));
     ((T*)a.out)[a.at(a.os, t, e / D) + e % D] = (T)NAN;
@@ -569,6 +571,7 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void tiles_kernel(Paged P
   const int split = (int)(rank / (uint32_t)a.tiles), tile = a.tiles - 1 - (int)(rank % (uint32_t)a.tiles);
   const int g = (int)(id % (uint32_t)P.hkv), b = (int)(id / (uint32_t)P.hkv);
   const Chunk ch = chunk_of(P, b);
+  if (!all_in_order(P, b)) return;
   if (is_bad(a, ch)) {
     if (split == 0 && tile == 0 && g == 0) fill_nan<T, X::D>(P, a, ch, b, X::NT);
     return;
@@ -606,6 +609,7 @@ template <typename T, typename X>
 __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void shares_kernel(Paged P, AttendArgs a) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[X::kLds];
   __shared__ uint64_t waves[X::W], found[2], kept[4];
+  __shared__ int broken_of[X::W];
   __shared__ int fix[3];
   no_fix(fix);
   const int tid = (int)threadIdx.x, lane = tid & 63;
@@ -617,10 +621,25 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void shares_kernel(Paged 
   const int per = few ? 1 : (P.B + X::NT - 1) / X::NT, b0 = min((few ? lane : tid) * per, P.B), b1 = min(b0 + per, P.B);
   Chunk own = {0, 0, 0, false};
   uint64_t mine = 0;
+  int broken = P.B;  // the first sequence whose chunk is not in order: it and all after it have no stages
   for (int b = b0; b < b1; ++b) {
     own = chunk_of(P, b);
+    if (!in_order(P, own.first, P.cu_q[b + 1])) {
+      broken = b;
+      break;
+    }
     mine += stages(own);
   }
+  if (few) {
+    const uint64_t all = __ballot(broken < P.B);
+    broken = all ? __builtin_ctzll(all) : P.B;
+  } else {
+    broken = min_across(broken);
+    if (lane == 0) broken_of[tid >> 6] = broken;
+    __syncthreads();
+    for (int w = 0; w < X::W; ++w) broken = min(broken, broken_of[w]);
+  }
+  if (b0 > broken) mine = 0;
   uint64_t upto = mine;  // with the stages of the sequences before
   for (int o = 1; o < 64; o <<= 1) {
     const uint64_t x = __shfl_up((unsigned long long)upto, o);
@@ -640,7 +659,7 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void shares_kernel(Paged 
   }
   total = uniform(total * heads);
   if (few ? __any(b0 < b1 && is_bad(a, own)) : true)
-    for (int b = (int)me; b < P.B; b += (int)gridDim.x) {
+    for (int b = (int)me; b < min(P.B, broken + 1); b += (int)gridDim.x) {
       const Chunk c = chunk_of(P, b);
       if (is_bad(a, c)) fill_nan<T, X::D>(P, a, c, b, X::NT);
     }
@@ -721,20 +740,8 @@ __global__ __launch_bounds__(256) void join_kernel(Paged P, AttendArgs a) {
   const uint32_t u = blockIdx.x * R + (uint32_t)tid / (64 * WAVES);
   const int t = (int)(u / (uint32_t)a.hq), h = (int)(u % (uint32_t)a.hq);
   bool live = t < P.T;
-  // the token's sequence; the lanes hold those of 64 and the one that is found hands its own out
-  Chunk ch = {0, 0, 0, false};
-  int b = 0;
-  for (int s = 0; s < P.B; s += 64) {
-    const int x = min(s + lane, P.B - 1);
-    const int32_t first = P.cu_q[x], end = P.cu_q[x + 1], kv = P.kv_len[x];
-    const int before = __popcll(__ballot(s + lane < P.B && end <= t));
-    b += before;
-    if (before < min(64, P.B - s)) {
-      ch = chunk_of(P, __builtin_amdgcn_readlane(first, before), __builtin_amdgcn_readlane(end, before),
-                    __builtin_amdgcn_readlane(kv, before));
-      break;
-    }
-  }
+  int b;
+  const Chunk ch = chunk_of_token(P, t, b);
   live = live && !is_bad(a, ch) && t >= ch.first && t < ch.first + ch.n;
   const int G = (int)a.group.d, g = (int)a.group.quot((uint32_t)h), r = (t - ch.first) * G + h - g * G;
   int from = 0, to = -1;

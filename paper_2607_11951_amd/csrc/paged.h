@@ -62,15 +62,50 @@ struct Chunk {
   int32_t first, n, kv;  // first token, new tokens, cached tokens with them
   bool ok;
 };
+// Whether a chunk's first token and end are in the packed arrays, in this order.  From the first chunk on that is not in
+// order all are bad: so chunks that are good follow one another, and no token belongs to two.
+__device__ inline bool in_order(const Paged& P, int32_t first, int32_t end) {
+  return first >= 0 && end >= first && end <= P.T;
+}
 __device__ inline Chunk chunk_of(const Paged& P, int32_t first, int32_t end, int32_t kv) {
   Chunk c;
   c.first = first;
   c.kv = kv;
-  c.ok = first >= 0 && end >= first && end <= P.T;
+  c.ok = in_order(P, first, end);
   c.n = c.ok ? end - first : 0;
   c.ok = c.ok && kv >= c.n && kv <= P.reach;
   return c;
 }
+// (by itself: the chunks before are not looked at)
 __device__ inline Chunk chunk_of(const Paged& P, int b) { return chunk_of(P, P.cu_q[b], P.cu_q[b + 1], P.kv_len[b]); }
+
+// Whether the chunks of sequences 0 .. n - 1 are in order.  A whole wave asks, 64 at a time.
+__device__ inline bool all_in_order(const Paged& P, int n) {
+  bool ok = true;
+  for (int s = 0; s < n; s += 64) {
+    const int x = min(s + (int)(threadIdx.x & 63), n - 1);
+    ok = ok && in_order(P, P.cu_q[x], P.cu_q[x + 1]);
+  }
+  return __all(ok);
+}
+
+// The sequence of token t, and its chunk: not ok if t belongs to none (t may also lie before the chunk).  A whole
+// wave asks for one token: the lanes hold the chunks of 64 sequences, and of the first that is not in order or ends after
+// t the lane hands its own out.
+__device__ inline Chunk chunk_of_token(const Paged& P, int t, int& b) {
+  const int lane = (int)threadIdx.x & 63;
+  for (b = 0; b < P.B; b += 64) {
+    const int x = min(b + lane, P.B - 1);
+    const int32_t first = P.cu_q[x], end = P.cu_q[x + 1], kv = P.kv_len[x];
+    const uint64_t stop = __ballot(b + lane < P.B && (end > t || !in_order(P, first, end)));
+    if (stop) {
+      const int i = __builtin_ctzll(stop);
+      b += i;
+      return chunk_of(P, __builtin_amdgcn_readlane(first, i), __builtin_amdgcn_readlane(end, i),
+                      __builtin_amdgcn_readlane(kv, i));
+    }
+  }
+  return {0, 0, 0, false};
+}
 
 }  // namespace grid
