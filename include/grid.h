@@ -687,7 +687,8 @@ size_t grid_attend_workspace_bytes(const grid_paged_cache* cache, const grid_chu
  * target's distribution.  A temperature that is not above 0, or no uniform and
  * no noise, is greedy: p is 1 at the largest logit (the lowest such index).
  * A row with no distribution (nothing allowed, or an allowed logit that is NaN or
- * +inf) accepts nothing and gives the token -1.
+ * +inf) accepts nothing and gives the token -1; so does one where noise that is not
+ * finite leaves no token a w / noise above 0 (noise is above 0 and finite).
  * tokens[b] = the accepted drafts, the next token, then -1; accepted[b] = a;
  * logprobs[b][j] = log p of tokens[b][j] (greedy: at temperature 1), 0 at -1.
  * draft_len is clamped to 0 .. K; a drafted id outside 0 .. V - 1 is refused.

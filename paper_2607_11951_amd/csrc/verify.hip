@@ -339,7 +339,10 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(VerifyArgs a) {
   if (!greedy && o.z > 0.f && at < n) {
     const int refused = a.draft[(int64_t)b * a.K + at];
     if (!a.probs) {
-      if (token < 0) token = refused;  // the draft was all that is allowed
+      // the draft was all that is allowed (noise that is not finite leaves no token too, whatever the draft is)
+      const bool is_allowed = (uint32_t)refused < (uint32_t)a.V &&
+                              (!masks || (masks[at * a.ms[1] + (refused >> 5)] >> (refused & 31) & 1));
+      if (token < 0 && is_allowed) token = refused;
     } else {
       // the race over this workgroup's part of what is left of row `at`
       const float* q = a.probs + b * a.ps[0] + at * a.ps[1];
