@@ -698,7 +698,7 @@ typedef struct {
   int32_t dtype;               /* GRID_DTYPE_F32, _BF16 or _F16 */
   int32_t B;                   /* 1 .. 65535 */
   int32_t K;                   /* 0 .. 63 */
-  int32_t V;                   /* >= 1 */
+  int32_t V;                   /* 1 .. 2^30 - 2048 */
   int64_t logits_stride[2];    /* sequence, row; in elements */
   const uint32_t* mask;        /* device rows of the mask layout, or NULL: all allowed */
   int64_t mask_stride[2];      /* sequence, row; in words */

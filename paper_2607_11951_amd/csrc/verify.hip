@@ -414,8 +414,10 @@ void plan(VerifyArgs& a, int steps) {
   a.races = (int32_t)(((int64_t)a.V + a.race - 1) / a.race);
 }
 
+// (tokens are counted in 32 bits past a row's end: to the end of the last piece, and of the races' last part, which begins
+// before V and is no longer than V and a step)
 bool sizes_ok(int32_t B, int32_t K, int32_t V) {
-  return B >= 1 && B <= 65535 && K >= 0 && K <= 63 && V >= 1 && V <= INT32_MAX - 2 * kStep;
+  return B >= 1 && B <= 65535 && K >= 0 && K <= 63 && V >= 1 && V <= (1 << 30) - kStep;
 }
 
 size_t head_bytes(int32_t B) { return ((size_t)B * 12 + 255) / 256 * 256; }

@@ -1,0 +1,29 @@
+"""Sizes at the limits of what the kernels of a model's step count in: refused on the host, before anything is enqueued.
+Through the C ABI, with addresses that are never read."""
+
+import ctypes
+
+import pytest
+
+from test_step_host import S, append, attend, cache, chunks, refused, verify  # noqa: F401
+
+by = ctypes.byref
+
+
+@pytest.mark.parametrize("V", [(1 << 30) - 2047, 1 << 30, (1 << 31) - 4096 - 1, (1 << 31) - 1])
+def test_vocabularies_are_counted_in_32_bits(S, V):  # noqa: F811
+    """the pieces of a row and the parts of the race end less than 2^31 after its start"""
+    assert S.lib().grid_verify_workspace_bytes(1, 0, V) == 0
+    refused(S, S.lib().grid_verify(by(verify(S, V=V, workspace_bytes=1 << 62)), None), "sizes")
+
+
+def test_the_largest_vocabulary(S):  # noqa: F811
+    V = (1 << 30) - 2048
+    assert S.lib().grid_verify_workspace_bytes(1, 0, V) > 0
+    for steps in (2, 4):  # of 2048 tokens, in a piece of float32 and of 16-bit rows
+        piece = steps * 2048
+        assert -(-V // piece) * piece < 1 << 31
+    for B in (1, 2, 3, 100, 700, 1024, 65535):
+        n = min(max(1, 1024 // B), -(-V // 2048))
+        race = -(-(-(-V // n)) // 2048) * 2048
+        assert -(-V // race) * race < 1 << 31
