@@ -803,6 +803,13 @@ __global__ __launch_bounds__(256) void join_kernel(Paged P, AttendArgs a) {
   if (a.lse && e == 0) a.lse[(int64_t)t * a.hq + h] = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
+// Keys that a sequence's rows are given, at most: with a window those of its chunk too, from a multiple of 128 on.
+int64_t span_of(const grid_paged_cache* c, const grid_chunks* x, const grid_attend_args* g) {
+  const int64_t span = std::min<int64_t>(g->max_kv, (int64_t)x->table_cols * c->page_size);
+  return g->window ? std::min<int64_t>(span, (int64_t)g->window + g->max_q + 127) : span;
+}
+constexpr int64_t kStage = 64;  // the shortest stage of the shares
+
 int check(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_attend_args* g, bool pointers) {
   const int rc = check_paged("grid_attend", cache, chunks, pointers);
   if (rc != GRID_OK) return rc;
@@ -816,6 +823,9 @@ int check(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_a
   if (!std::isfinite(g->scale)) return bad("scale");
   if ((int64_t)std::min(g->max_q, chunks->n_tokens) * (g->n_heads / cache->n_kv_heads) >= 1 << 30)
     return fail(GRID_E_CAPACITY, "grid_attend: 2^30 rows of a sequence and key head or more");
+  // (the shares count the stages of a sequence, all key heads together, in 32 bits)
+  if ((span_of(cache, chunks, g) + kStage - 1) / kStage * cache->n_kv_heads >= (int64_t)1 << 32)
+    return fail(GRID_E_CAPACITY, "grid_attend: 2^38 keys of a sequence in all key heads or more");
   if (!pointers || chunks->n_tokens == 0) return GRID_OK;
   if (!g->q || !g->out) return bad("null pointer");
   if (!rows_fit(g->q, g->q_stride, 2) || !rows_fit(g->out, g->out_stride, 2))
@@ -851,8 +861,7 @@ Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_atten
   Shape s;
   const int group = g->n_heads / c->n_kv_heads;
   const int64_t rows = (int64_t)std::min(g->max_q, std::max(1, x->n_tokens)) * group;
-  int64_t span = std::min<int64_t>(g->max_kv, (int64_t)x->table_cols * c->page_size);
-  if (g->window) span = std::min<int64_t>(span, (int64_t)g->window + g->max_q + 127);
+  const int64_t span = span_of(c, x, g);
   const int64_t heads = (int64_t)c->n_kv_heads * x->n_seqs;
   const int64_t small = heads * ((rows + 31) / 32);  // tiles of 32
   const int few_keys = rows > 64                   ? 1024
@@ -870,7 +879,7 @@ Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_atten
   s.len = INT32_MAX;
   s.at_once = (c->head_dim == 256 ? 1 : 2) * kComputeUnits;
   if (s.shares) {
-    const int64_t stage = 64, stages = (span + stage - 1) / stage;
+    const int64_t stages = (span + kStage - 1) / kStage;
     s.blocks = std::min<int64_t>(heads * stages, 2 * kComputeUnits);
     s.join = stages > 1;
     s.parts = s.blocks / heads;

@@ -27,3 +27,23 @@ def test_the_largest_vocabulary(S):  # noqa: F811
         n = min(max(1, 1024 // B), -(-V // 2048))
         race = -(-(-(-V // n)) // 2048) * 2048
         assert -(-V // race) * race < 1 << 31
+
+
+def test_stages_of_a_sequence_are_counted_in_32_bits(S):  # noqa: F811
+    """64 keys a stage and key head: 2^38 keys in all heads are too many, as bounds or as a window's span; fewer are not"""
+    c = cache(S, n_kv_heads=1024, page_size=65536, head_dim=64)
+    x = chunks(S, table_cols=8192, table_stride=8192)
+
+    def both(**kw):
+        a = attend(S, n_heads=1024, **kw)
+        size = S.lib().grid_attend_workspace_bytes(by(c), by(x), by(a))
+        a.workspace = None  # refused at the latest for this
+        return size, S.lib().grid_attend(by(c), by(x), by(a), None)
+
+    for kw in (dict(max_kv=1 << 28), dict(max_kv=1 << 29), dict(max_kv=(1 << 28) - 63),
+               dict(max_kv=1 << 30, window=1 << 28)):
+        assert both(**kw) == (0, -11), kw  # GRID_E_CAPACITY
+        assert "keys" in S.lib().grid_last_error().decode()
+    for kw in (dict(max_kv=(1 << 28) - 64), dict(max_kv=1 << 30, window=1 << 27)):
+        size, rc = both(**kw)
+        assert size > 0 and rc == -1, kw
