@@ -647,7 +647,9 @@ int grid_kv_append(const grid_paged_cache* cache, const grid_chunks* chunks, con
  *   lse[t][h] = log of the sum over s of exp(scale * q[t][h] . K[s]).
  * Scores, softmax and sums are held in 32 bits; the weights are rounded to the
  * dtype before they multiply V, the result once at the end.  What a token does
- * not see has no part in its result, infinities and NaN there included.
+ * not see has no part in its result, infinities and NaN there included, and
+ * neither have the block table's entries of pages that no token of a chunk sees
+ * (those of pages that a window has left behind may be out of range).
  * max_q and max_kv bound the chunks' lengths and kv_len; they fix the launch.
  * The rows of a sequence that is bad or longer than they say are NaN, and so
  * are those that would read a page that is not in the cache (others of that

@@ -173,8 +173,8 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
   const int pos_max = first_pos + (int)a.group.quot((uint32_t)min(r0 + 31, rows - 1));
 
   // Loads.  Load i of a wave brings RPI rows from row WR * wave + i * RPI of the stage on, a lane piece `lane % PR` of
-  // row `lane / PR`.  At and after s_hi come rows that the same page holds, or the last ones again: nothing
-  // is made of them, whatever they hold.
+  // row `lane / PR`.  At and after s_hi come rows that the same page holds, or the last ones again, and before s_seen, the
+  // first key that a row of the tile sees, page 0 where the table has no page: nothing is made of them, whatever they hold.
   const uint32_t base = (uint32_t)(uintptr_t)(GRID_LDS uint8_t*)lds;
   const uint16_t *kg = P.k + (uint64_t)g * P.ks[2], *vg = P.v + (uint64_t)g * P.vs[2];
   const auto* table = (const __attribute__((address_space(4))) int32_t*)(P.table + (int64_t)b * P.table_stride);
@@ -183,19 +183,22 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_>::run(cons
   int32_t page[FIND];
   uint32_t row[FIND];
   bool missing = false;
+  const int s_seen = a.window ? first_pos + (int)a.group.quot((uint32_t)(tile * TM)) - a.window + 1 : 0;
   const auto find = [&](int s0) {
+    const auto key = [&](int i) {
+      const int s = s0 + wave * WR + (UNI ? i * RUN : i * RPI + lrow);
+      return UNI ? min(s, (s_hi - 1) & ~(RUN - 1)) : min(s, s_hi - 1);
+    };
 #pragma unroll
     for (int i = 0; i < FIND; ++i) {
-      const int s = s0 + wave * WR + (UNI ? i * RUN : i * RPI + lrow);
-      const uint32_t at = (uint32_t)(UNI ? min(s, (s_hi - 1) & ~(RUN - 1)) : min(s, s_hi - 1));
-      const uint32_t c = P.page.quot(at);
+      const uint32_t at = (uint32_t)key(i), c = P.page.quot(at);
       row[i] = at - c * P.page.d;
       page[i] = table[c];
     }
 #pragma unroll
     for (int i = 0; i < FIND; ++i) {
       const bool in = P.in_cache(page[i]);
-      missing |= !in;
+      missing |= !in && key(i) + (UNI ? RUN : 1) > s_seen;
       page[i] = in ? page[i] : 0;
     }
   };
