@@ -6,6 +6,8 @@
 //
 // Bound by bytes, for few tokens by dependent reads: 8 chunks of up to 2048 tokens, 32 + 8 + 8 heads of 128 in float16,
 // half of each rotated, take 55.5 us, 4.5 TB/s (a copy reaches 5.09); one token 3.2 us on the device.
+#include <algorithm>
+
 #include "lanes.h"
 #include "paged.h"
 
@@ -24,6 +26,7 @@ struct AppendArgs {
   int32_t hq, n_positions, half, interleaved;  // half = rot_dim / 2
   float eps, over;  // over = 1 / head_dim
   int32_t lanes;  // lanes of a head's vector
+  int32_t base;   // the launch's first workgroup among all
 };
 
 template <typename T>
@@ -51,7 +54,7 @@ enum class Turn { kNone, kHalves, kPairs };
 // read once.
 template <typename T, Turn TURN, bool NORM>
 __global__ __launch_bounds__(kThreads) void append_kernel(Paged P, AppendArgs a) {
-  const int t = (int)blockIdx.x, tid = (int)threadIdx.x, lane = tid & 63;
+  const int t = (int)blockIdx.x + a.base, tid = (int)threadIdx.x, lane = tid & 63;
   if (t >= P.T) {
     const int b = (t - P.T) * kThreads + tid;
     __shared__ int broken;  // the first of the sequences up to here whose chunk is not in order
@@ -226,12 +229,16 @@ extern "C" int grid_kv_append(const grid_paged_cache* cache, const grid_chunks* 
   a.lanes = 1;
   while (a.lanes * 8 < D) a.lanes *= 2;
   const Paged P = make_paged(cache, chunks);
-  const int blocks = P.T + (g.status ? (P.B + kThreads - 1) / kThreads : 0);
+  // (a launch has less than 2^32 threads, 2^24 workgroups)
+  const int blocks = P.T + (g.status ? (P.B + kThreads - 1) / kThreads : 0), most = 1 << 23;
   if (blocks == 0) return GRID_OK;
-  if (cache->dtype == GRID_DTYPE_BF16)
-    launch<bf16_t>(P, a, (unsigned)blocks, (hipStream_t)stream);
-  else
-    launch<f16_t>(P, a, (unsigned)blocks, (hipStream_t)stream);
+  for (a.base = 0; a.base < blocks; a.base += most) {
+    const unsigned n = (unsigned)std::min(blocks - a.base, most);
+    if (cache->dtype == GRID_DTYPE_BF16)
+      launch<bf16_t>(P, a, n, (hipStream_t)stream);
+    else
+      launch<f16_t>(P, a, n, (hipStream_t)stream);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(GRID_E_HIP, std::string("grid_kv_append launch: ") + hipGetErrorString(e));
   return GRID_OK;
