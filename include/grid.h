@@ -654,7 +654,8 @@ int grid_kv_append(const grid_paged_cache* cache, const grid_chunks* chunks, con
  * The rows of a sequence that is bad or longer than they say are NaN, and so
  * are those that would read a page that is not in the cache (others of that
  * sequence may be).  GRID_E_CAPACITY: 2^30 rows (tokens times query heads of a
- * key head) of a sequence, or 2^38 keys times key heads.  Rows of tokens that belong to no sequence are left as they
+ * key head) of a sequence, 2^38 keys times key heads, or more than 2^23 tiles of 128
+ * rows or, of chunks of up to 64 rows, tokens times heads.  Rows of tokens that belong to no sequence are left as they
  * are.
  * Workspace: device scratch, 16-byte aligned, of at least
  * grid_attend_workspace_bytes; nothing is expected in it. */

@@ -62,7 +62,7 @@ struct AttendArgs {
   int2* runs;       // [sequences][key heads]: first and last workgroup of the unit (few rows)
   Divisor group;
   int32_t hq, max_q, max_kv, window;
-  // many rows: workgroups; tiles a sequence and key head, ranges of len keys (whole stages); units side by side
+  // many rows: workgroups; tiles a sequence and key head, ranges of len keys (whole stages); units side by side (kPacked)
   int32_t blocks, tiles, splits, len, bundle;
   float c;                     // |scale| * log2 e, above 0
   bool negate;                 // scale < 0: the queries are negated
@@ -71,6 +71,8 @@ struct AttendArgs {
     return (uint64_t)t * stride[0] + (uint64_t)h * stride[1];
   }
 };
+
+constexpr int kPacked = -1;
 
 constexpr float kLn2 = 0.693147180559945309417f, kLog2e = 1.44269504088896340736f;
 
@@ -549,8 +551,26 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void tiles_kernel(Paged P
   // Workgroups are dealt to the 8 dies in turn; a die is to read the same keys for the tiles that it runs together.  A unit
   // is a sequence and key head.
   const uint32_t per = (uint32_t)(a.tiles * a.splits);
-  uint32_t id, rank;
-  if (a.bundle == 0) {
+  uint32_t id = 0, rank = 0;
+  int split = 0, tile, g, b;
+  if (a.bundle == kPacked) {
+    // Many sequences of which few have many rows: workgroups are numbered by the rows there are.  The tiles of sequence b are
+    // numbers cu_q[b] * group / TM + b (rounded down) and on; for a chunk of n tokens the next sequence's begin n * group / TM,
+    // rounded down, and 1 later at least, so after its last.  The sequence is the last whose numbers begin at or before this one.
+    if (blockIdx.x >= (uint32_t)a.blocks) return;
+    const int lane = (int)threadIdx.x & 63, G = (int)a.group.d, u = (int)(blockIdx.x / (uint32_t)P.hkv);
+    g = (int)(blockIdx.x % (uint32_t)P.hkv);
+    uint64_t stop = 0;
+    for (b = 0; b < P.B && !stop; b += 64) {
+      const int x = min(b + lane, P.B - 1);
+      const int32_t first = P.cu_q[x], end = P.cu_q[x + 1];
+      stop = __ballot(b + lane < P.B && (!in_order(P, first, end) || end * G / X::TM + x + 1 > u));
+    }
+    if (!stop) return;
+    b += __builtin_ctzll(stop) - 64;
+    tile = u - min(max(P.cu_q[b], 0), P.T) * G / X::TM - b;
+    if (tile < 0) return;  // before the first sequence
+  } else if (a.bundle == 0) {
     // Many units that all run at once: runs of 16 that follow one another go to one die, so that the keys are shared and chunks of many
     // tiles spread over the dies; every other round of the dies is reversed, for a unit's tiles come the longest first
     // (7 chunks of up to 77 tokens, a window of 300, 5 key heads: 8.2 us; with a unit a die 9.2, with an eighth of them all
@@ -571,10 +591,14 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void tiles_kernel(Paged P
     rank = in / side;
     id = first + in - rank * side;
   }
-  const int split = (int)(rank / (uint32_t)a.tiles), tile = a.tiles - 1 - (int)(rank % (uint32_t)a.tiles);
-  const int g = (int)(id % (uint32_t)P.hkv), b = (int)(id / (uint32_t)P.hkv);
+  if (a.bundle != kPacked) {
+    split = (int)(rank / (uint32_t)a.tiles);
+    tile = a.tiles - 1 - (int)(rank % (uint32_t)a.tiles);
+    g = (int)(id % (uint32_t)P.hkv);
+    b = (int)(id / (uint32_t)P.hkv);
+    if (!all_in_order(P, b)) return;
+  }
   const Chunk ch = chunk_of(P, b);
-  if (!all_in_order(P, b)) return;
   if (is_bad(a, ch)) {
     if (split == 0 && tile == 0 && g == 0) fill_nan<T, X::D>(P, a, ch, b, X::NT);
     return;
@@ -843,6 +867,7 @@ int check(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_a
 //  - More rows: tiles of 128; where they are fewer than 3/4 of the workgroups that run at once the keys are split, into
 //    ranges of at least 512 (a chunk after a cache, 6144 keys together, 28 heads on 4 of 128: of 1280 tokens 148 us split
 //    and 160 whole, of 2048, 7/8 of the workgroups, 202 and 175).
+//    Where sequences times the tiles of the longest chunk exceed a launch, workgroups are numbered by the rows there are.
 //  - Few keys, where tiles of 32 run all at once: those, a workgroup each for all its keys.  Four waves share a tile's
 //    keys, and nothing needs joining.  Up to 64 rows that saves the joining launch and costs the keys in turn: a token of 28
 //    heads on 4 of 128 after 256 keys takes 7.0 us so and 10.2 shared, after 512 9.4 and 10.6, after 1024 14.6 and 10.4;
@@ -852,10 +877,11 @@ int check(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_a
 //    keys they would be read too often: 14 times for 4 chunks of 64 tokens after 8192 with 7 heads a key head, that tiles of
 //    128, split, take 61 us for.
 constexpr int kComputeUnits = 256;
+constexpr int64_t kMostBlocks = (int64_t)1 << 23;  // of a launch: below 2^32 threads
 struct Shape {
   int tm, splits, len;
   int64_t tiles, blocks;
-  bool shares, join;
+  bool shares, join, packed;
   int64_t at_once;  // workgroups that run side by side (many rows)
   int64_t parts;  // of a row, at most but for one or two
   size_t slots;   // of parts
@@ -874,6 +900,7 @@ Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_atten
                                                     : 640;
   const bool narrow = small <= 2 * kComputeUnits && span <= few_keys;
   s.shares = rows <= 64 && !narrow;
+  s.packed = false;
   s.tm = rows <= 32 || narrow ? 32
          : rows <= 64                                                                                  ? 64
                                                                                                        : 128;
@@ -898,6 +925,10 @@ Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_atten
       s.len = (int)(((span + s.splits - 1) / s.splits + 127) / 128 * 128);
       s.blocks *= s.splits;
     }
+  }
+  if (s.blocks > kMostBlocks) {
+    s.packed = true;
+    s.blocks = c->n_kv_heads * ((int64_t)x->n_tokens * group / s.tm + x->n_seqs);
   }
   s.join = s.splits > 1;
   s.parts = s.splits;
@@ -982,7 +1013,7 @@ extern "C" int grid_attend(const grid_paged_cache* cache, const grid_chunks* chu
   if (!args->workspace || (uintptr_t)args->workspace % 16 != 0 ||
       args->workspace_bytes < workspace_of(cache, chunks, s))
     return fail(GRID_E_ARG, "grid_attend: workspace too small or not aligned");
-  if (s.blocks > (int64_t)1 << 23 || (s.join && (int64_t)chunks->n_tokens * args->n_heads > (int64_t)1 << 23))
+  if (s.blocks > kMostBlocks || (s.join && (int64_t)chunks->n_tokens * args->n_heads > kMostBlocks))
     return fail(GRID_E_CAPACITY, "grid_attend: too many rows for one launch");
   AttendArgs a;
   a.q = (const uint16_t*)args->q;
@@ -1008,7 +1039,10 @@ extern "C" int grid_attend(const grid_paged_cache* cache, const grid_chunks* chu
   a.len = s.len;
   // as many units side by side as fill the chip
   const int64_t per = s.tiles * s.splits, units = s.blocks / per, fill = (s.at_once + per - 1) / per;
-  a.bundle = s.blocks <= s.at_once && units > 8 ? 0 : (int32_t)std::min<int64_t>(units, (fill + 7) / 8 * 8);
+  if (s.packed)
+    a.bundle = kPacked;
+  else
+    a.bundle = s.blocks <= s.at_once && units > 8 ? 0 : (int32_t)std::min<int64_t>(units, (fill + 7) / 8 * 8);
   a.negate = args->scale < 0.f;
   a.c = std::fmin(std::fmax(std::fabs(args->scale) * kLog2e, 1e-30f), 1e30f);
   const Paged P = make_paged(cache, chunks);

@@ -47,3 +47,11 @@ def test_stages_of_a_sequence_are_counted_in_32_bits(S):  # noqa: F811
     for kw in (dict(max_kv=(1 << 28) - 64), dict(max_kv=1 << 30, window=1 << 27)):
         size, rc = both(**kw)
         assert size > 0 and rc == -1, kw
+
+
+def test_tiles_are_counted_by_rows(S):  # noqa: F811
+    """a launch has 2^23 workgroups: rows that need more are refused, before anything is enqueued"""
+    c = cache(S, n_kv_heads=1024, head_dim=64, k_stride=S._THREE(1 << 20, 1 << 16, 64), v_stride=S._THREE(1 << 20, 1 << 16, 64))
+    a = attend(S, n_heads=1024, max_q=1 << 24, max_kv=80)
+    rc = S.lib().grid_attend(by(c), by(chunks(S, n_tokens=1 << 24)), by(a), None)
+    assert rc == -11 and "rows" in S.lib().grid_last_error().decode()
