@@ -7,11 +7,14 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
+#include <initializer_list>
 #include <stdexcept>
 #include <string>
 
@@ -122,6 +125,19 @@ void* stream_of(at::Device dev) {
   return (void*)c10::hip::getCurrentHIPStream(dev.index()).stream();
 }
 
+// The calls have no derivatives: tensors that want one are refused while torch records them, backward or forward.
+void no_gradient(std::initializer_list<const at::Tensor*> tensors) {
+  const bool back = c10::GradMode::is_enabled(), forward = c10::AutogradState::get_tls_state().get_fw_grad_mode();
+  for (const at::Tensor* t : tensors)
+    if (t && ((back && t->requires_grad()) || (forward && t->_fw_grad(0).defined())))
+      throw Refused(PyExc_RuntimeError, "there are no gradients of this call: detach its tensors, or call it under torch.no_grad()");
+}
+// What a call has written in place, for torch to know.
+void written(std::initializer_list<const at::Tensor*> tensors) {
+  for (const at::Tensor* t : tensors)
+    if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
+
 PyObject* given(PyObject* o, const at::Tensor& made) {
   if (o == Py_None) return THPVariable_Wrap(made);
   Py_INCREF(o);
@@ -149,7 +165,8 @@ PyObject* guarded(Py_ssize_t n, Py_ssize_t want, F f) {
 PyObject* kv_append(PyObject*, PyObject* const* x, Py_ssize_t n) {
   return guarded(n, 16, [&]() -> PyObject* {
     const at::Tensor &k = tensor(x[0], "k"), &v = tensor(x[1], "v"), &k_pages = tensor(x[2], "k_pages");
-    const grid_paged_cache c = paged(k_pages, tensor(x[3], "v_pages"));
+    const at::Tensor& v_pages = tensor(x[3], "v_pages");
+    const grid_paged_cache c = paged(k_pages, v_pages);
     const at::Device dev = k_pages.device();
     const at::ScalarType type = k_pages.scalar_type();
     const int64_t D = c.head_dim, tokens = k.dim() ? k.size(0) : 0;
@@ -181,12 +198,14 @@ PyObject* kv_append(PyObject*, PyObject* const* x, Py_ssize_t n) {
     a.k_norm = ptr<float>(k_norm);
     a.eps = real(x[14], "eps");
     a.status = ptr<int32_t>(status);
+    const at::Tensor* q_out = maybe(x[8], "q_out");
+    no_gradient({&k, &v, &k_pages, &v_pages, q, q_out, cos, sin, q_norm, k_norm});
     void* stream = stream_of(dev);
     const c10::DeviceGuard guard(dev);
     at::Tensor out;
     if (q) {
       vectors(*q, type, tokens, D, dev, a.q_stride, "q");
-      out = x[8] == Py_None ? at::empty(q->sizes(), q->options()) : tensor(x[8], "q_out");
+      out = q_out ? *q_out : at::empty(q->sizes(), q->options());
       vectors(out, type, tokens, D, dev, a.q_out_stride, "q_out");
       need(out.size(1) == q->size(1), "q_out has the shape of q");
       a.q = ptr(*q);
@@ -195,6 +214,7 @@ PyObject* kv_append(PyObject*, PyObject* const* x, Py_ssize_t n) {
     }
     const int rc = grid_kv_append(&c, &ch, &a, stream);
     if (rc != GRID_OK) return PyLong_FromLong(rc);
+    written({&k_pages, &v_pages, q ? q_out : nullptr, status});
     PyObject* first = q ? given(x[8], out) : (Py_INCREF(Py_None), Py_None);
     PyObject* both = PyTuple_Pack(2, first, x[15]);
     Py_DECREF(first);
@@ -205,8 +225,8 @@ PyObject* kv_append(PyObject*, PyObject* const* x, Py_ssize_t n) {
 // q, k_pages, v_pages, block_table, kv_len, cu_q, max_q, max_kv, scale, window, out, lse, workspace
 PyObject* attend(PyObject*, PyObject* const* x, Py_ssize_t n) {
   return guarded(n, 13, [&]() -> PyObject* {
-    const at::Tensor &q = tensor(x[0], "q"), &k_pages = tensor(x[1], "k_pages");
-    const grid_paged_cache c = paged(k_pages, tensor(x[2], "v_pages"));
+    const at::Tensor &q = tensor(x[0], "q"), &k_pages = tensor(x[1], "k_pages"), &v_pages = tensor(x[2], "v_pages");
+    const grid_paged_cache c = paged(k_pages, v_pages);
     const at::Device dev = k_pages.device();
     const int64_t D = c.head_dim, tokens = q.dim() ? q.size(0) : 0;
     const grid_chunks ch =
@@ -221,24 +241,25 @@ PyObject* attend(PyObject*, PyObject* const* x, Py_ssize_t n) {
     a.window = whole(x[9], "window");
     const at::Tensor* given_lse = maybe(x[11], "lse");
     dense(given_lse, at::kFloat, {tokens, q.size(1)}, dev, "lse");
+    const at::Tensor *given_out = maybe(x[10], "out"), *given_work = maybe(x[12], "workspace");
+    no_gradient({&q, &k_pages, &v_pages, given_out, given_lse});
     void* stream = stream_of(dev);
     const c10::DeviceGuard guard(dev);
-    const at::Tensor out = x[10] == Py_None ? at::empty(q.sizes(), q.options()) : tensor(x[10], "out");
+    const at::Tensor out = given_out ? *given_out : at::empty(q.sizes(), q.options());
     vectors(out, q.scalar_type(), tokens, D, dev, a.out_stride, "out");
     need(out.size(1) == q.size(1), "out has the shape of q");
     const at::Tensor lse = given_lse ? *given_lse : at::empty({tokens, q.size(1)}, q.options().dtype(at::kFloat));
     a.out = ptr(out);
     a.lse = ptr<float>(lse);
-    at::Tensor work;
-    if (x[12] == Py_None)
-      work = at::empty({(int64_t)grid_attend_workspace_bytes(&c, &ch, &a)}, q.options().dtype(at::kByte));
-    else
-      work = tensor(x[12], "workspace");
+    const at::Tensor work =
+        given_work ? *given_work
+                   : at::empty({(int64_t)grid_attend_workspace_bytes(&c, &ch, &a)}, q.options().dtype(at::kByte));
     need(work.device() == dev && work.is_contiguous(), "workspace: a contiguous tensor on the cache's device");
     a.workspace = ptr(work);
     a.workspace_bytes = work.nbytes();
     const int rc = grid_attend(&c, &ch, &a, stream);
     if (rc != GRID_OK) return PyLong_FromLong(rc);
+    written({given_out, given_lse, given_work});
     PyObject *o = given(x[10], out), *l = given(x[11], lse), *both = PyTuple_Pack(2, o, l);
     Py_DECREF(o);
     Py_DECREF(l);
@@ -300,13 +321,15 @@ PyObject* verify(PyObject*, PyObject* const* x, Py_ssize_t n) {
     dense(t, at::kInt, {B, K + 1}, dev, "tokens");
     dense(c, at::kInt, {B}, dev, "accepted");
     dense(l, at::kFloat, {B, K + 1}, dev, "logprobs");
+    const at::Tensor* given_work = maybe(x[11], "workspace");
+    no_gradient({&logits, probs, uniform, noise, temperature, l});
     void* stream = stream_of(dev);
     const c10::DeviceGuard guard(dev);
     const auto ints = logits.options().dtype(at::kInt);
     const at::Tensor tokens = t ? *t : at::empty({B, K + 1}, ints), accepted = c ? *c : at::empty({B}, ints);
     const at::Tensor logprobs = l ? *l : at::empty({B, K + 1}, ints.dtype(at::kFloat));
-    const at::Tensor work = x[11] == Py_None ? at::empty({(int64_t)grid_verify_workspace_bytes(a.B, a.K, a.V)}, ints.dtype(at::kByte))
-                                             : tensor(x[11], "workspace");
+    const at::Tensor work =
+        given_work ? *given_work : at::empty({(int64_t)grid_verify_workspace_bytes(a.B, a.K, a.V)}, ints.dtype(at::kByte));
     need(work.device() == dev && work.is_contiguous(), "workspace: a contiguous tensor on the logits' device");
     a.tokens = ptr<int32_t>(tokens);
     a.accepted = ptr<int32_t>(accepted);
@@ -315,6 +338,7 @@ PyObject* verify(PyObject*, PyObject* const* x, Py_ssize_t n) {
     a.workspace_bytes = work.nbytes();
     const int rc = grid_verify(&a, stream);
     if (rc != GRID_OK) return PyLong_FromLong(rc);
+    written({t, c, l, given_work});
     PyObject *p = given(x[8], tokens), *q = given(x[9], accepted), *r = given(x[10], logprobs);
     PyObject* all = PyTuple_Pack(3, p, q, r);
     Py_DECREF(p);

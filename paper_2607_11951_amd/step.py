@@ -5,7 +5,8 @@ contracts are in include/grid.h).  Arrays of chunks are packed: sequence b's new
 q, k and v; kv_len[b] counts the sequence's cached tokens with the chunk; position s of sequence b is row s % page_size
 of page block_table[b, s // page_size].  Pages are [pages, page_size, heads, head_dim] of any strides with dense vectors.
 
-Calls run on `stream`, or on the current stream; outputs and workspaces that are not given are allocated there.
+Calls run on `stream`, or on the current stream; outputs and workspaces that are not given are allocated there.  They have
+no gradients: tensors that require one are refused while torch records them.
 """
 
 import torch  # before _step, which links its libraries
