@@ -1,4 +1,5 @@
-"""Builds libgrid.so in-tree (host C++ with g++, kernels with hipcc for gfx950) and the Python module _step on it."""
+"""Builds libgrid.so in-tree (host C++ with g++, kernels with hipcc for gfx950) and, where torch is installed, the Python
+module _step on it."""
 
 import importlib.util
 import os
@@ -30,14 +31,16 @@ def build(verbose=False, jobs=8):
     objs = []
     procs = []
     # torch's headers and libraries, found without importing it
-    torch = Path(importlib.util.find_spec("torch").origin).parent
-    step = BUILD / "step_module.cpp.o"
-    cmd = ["g++", *HOST_FLAGS, "-D__HIP_PLATFORM_AMD__=1", "-isystem", torch / "include",
-           "-isystem", sysconfig.get_paths()["include"], "-isystem", "/opt/rocm/include", "-c", CSRC / "step_module.cpp",
-           "-o", step]
-    if verbose:
-        print(" ".join(str(c) for c in cmd), flush=True)
-    procs.append(subprocess.Popen([str(c) for c in cmd]))
+    spec = importlib.util.find_spec("torch")
+    if spec is not None:
+        torch = Path(spec.origin).parent
+        step = BUILD / "step_module.cpp.o"
+        cmd = ["g++", *HOST_FLAGS, "-D__HIP_PLATFORM_AMD__=1", "-isystem", torch / "include",
+               "-isystem", sysconfig.get_paths()["include"], "-isystem", "/opt/rocm/include", "-c",
+               CSRC / "step_module.cpp", "-o", step]
+        if verbose:
+            print(" ".join(str(c) for c in cmd), flush=True)
+        procs.append(subprocess.Popen([str(c) for c in cmd]))
     for src in HOST_SOURCES:
         obj = BUILD / (src + ".o")
         cmd = ["g++", *HOST_FLAGS, "-c", CSRC / src, "-o", obj]
@@ -58,10 +61,11 @@ def build(verbose=False, jobs=8):
     tmp = str(OUT) + ".tmp"
     _run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-pthread", "-o", tmp, *objs], verbose)
     os.replace(tmp, OUT)
-    tmp = str(MODULE) + ".tmp"
-    _run(["g++", "-shared", "-fPIC", "-o", tmp, step, f"-L{PKG}", "-l:libgrid.so", f"-L{torch / 'lib'}", "-ltorch_python",
-          "-ltorch_cpu", "-lc10", "-lc10_hip", "-Wl,-rpath,$ORIGIN"], verbose)
-    os.replace(tmp, MODULE)
+    if spec is not None:
+        tmp = str(MODULE) + ".tmp"
+        _run(["g++", "-shared", "-fPIC", "-o", tmp, step, f"-L{PKG}", "-l:libgrid.so", f"-L{torch / 'lib'}",
+              "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip", "-Wl,-rpath,$ORIGIN"], verbose)
+        os.replace(tmp, MODULE)
     return OUT
 
 
