@@ -63,6 +63,14 @@ float real(PyObject* o, const char* what) {
   }
   return (float)x;
 }
+bool truth(PyObject* o, const char* what) {
+  const int x = PyObject_IsTrue(o);
+  if (x < 0) {
+    PyErr_Clear();
+    throw Refused(PyExc_TypeError, std::string(what) + ": true or false is wanted");
+  }
+  return x != 0;
+}
 
 void dense(const at::Tensor* t, at::ScalarType type, at::IntArrayRef shape, at::Device dev, const char* name) {
   if (!t) return;
@@ -189,7 +197,7 @@ PyObject* kv_append(PyObject*, PyObject* const* x, Py_ssize_t n) {
     }
     a.cos = ptr<float>(cos);
     a.sin = ptr<float>(sin);
-    a.interleaved = PyObject_IsTrue(x[11]) == 1;
+    a.interleaved = truth(x[11], "interleaved");
     const at::Tensor *q_norm = maybe(x[12], "q_norm"), *k_norm = maybe(x[13], "k_norm"), *status = maybe(x[15], "status");
     dense(q_norm, at::kFloat, {D}, dev, "q_norm");
     dense(k_norm, at::kFloat, {D}, dev, "k_norm");

@@ -55,3 +55,13 @@ def test_tiles_are_counted_by_rows(S):  # noqa: F811
     a = attend(S, n_heads=1024, max_q=1 << 24, max_kv=80)
     rc = S.lib().grid_attend(by(c), by(chunks(S, n_tokens=1 << 24)), by(a), None)
     assert rc == -11 and "rows" in S.lib().grid_last_error().decode()
+
+
+def test_a_style_that_is_neither_true_nor_false(S):  # noqa: F811
+    """an error raised while the argument is read is the call's own, not left behind a result"""
+    torch = pytest.importorskip("torch")
+    pages, table = torch.zeros(4, 16, 2, 64, dtype=torch.bfloat16), torch.zeros(3, 5, dtype=torch.int32)
+    k, lens, cu = torch.zeros(7, 2, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)
+    for bad in (torch.zeros(2), torch.zeros(0, 3)):
+        with pytest.raises(TypeError, match="interleaved"):
+            S.G.kv_append(k, k, pages, pages, table, lens, cu, interleaved=bad)
