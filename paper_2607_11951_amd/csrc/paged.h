@@ -79,15 +79,26 @@ __device__ inline Chunk chunk_of(const Paged& P, int32_t first, int32_t end, int
 // (by itself: the chunks before are not looked at)
 __device__ inline Chunk chunk_of(const Paged& P, int b) { return chunk_of(P, P.cu_q[b], P.cu_q[b + 1], P.kv_len[b]); }
 
-// Whether the chunks of sequences 0 .. n - 1 are in order.  A whole wave asks, 64 at a time.
-__device__ inline bool all_in_order(const Paged& P, int n) {
-  bool ok = true;
-  for (int s = 0; s < n; s += 64) {
-    const int x = min(s + (int)(threadIdx.x & 63), n - 1);
-    ok = ok && in_order(P, P.cu_q[x], P.cu_q[x + 1]);
+// Whether the chunks of the sequences before b are in order, as `all` threads find together of whom this is the one
+// `tid`: the first entries are asked for at once, and what is found is told later.  (Entries that do not decrease are in
+// order but for the first and the last; where that is past the rows b's own chunk is out of order too, and has no rows.)
+struct OrderBefore {
+  int32_t zeroth, x, next;
+  __device__ OrderBefore(const Paged& P, int b, int tid)
+      : zeroth(P.cu_q[0]), x(P.cu_q[min(tid, b)]), next(P.cu_q[min(tid + 1, b)]) {}
+  __device__ bool ok(const Paged& P, int b, int tid, int all) const {
+    bool down = x > next || (b > 0 && zeroth < 0);
+#pragma unroll 4
+    for (int s = all + 4 * tid; s < b; s += 4 * all) {
+      const int32_t* at = P.cu_q + min(s, b - 4);
+      int32_t y[4];
+      __builtin_memcpy(y, at, 16);
+      const int32_t last = at[4];
+      down |= (y[0] > y[1]) | (y[1] > y[2]) | (y[2] > y[3]) | (y[3] > last);
+    }
+    return !down;
   }
-  return __all(ok);
-}
+};
 
 // The sequence of token t, and its chunk: not ok if t belongs to none (t may also lie before the chunk).  A whole
 // wave asks for one token: the lanes hold the chunks of 64 sequences, and of the first that is not in order or ends after
