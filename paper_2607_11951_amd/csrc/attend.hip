@@ -11,10 +11,11 @@
 // rows are read, transposed on the way from LDS, in the order the scores lie in.
 //
 // Bounds (bf16, heads of 128; a copy reaches 5.09 TB/s here, a product of 8192^3 1392 TFLOP/s).  Few rows read the cache
-// once: 64 sequences of up to 8192 keys, 8 key heads, one token each, take 181 us, 4.97 TB/s of it; 32 of up to 4096, 4 key
-// heads, up to 5 tokens, 44 us, 3.1 TB/s (34 the shares, 8 stages each, 5 the joining); one of 1500 keys 11 us, two launches
+// once: 64 sequences of up to 8192 keys, 8 key heads, one token each, take 183 us, 4.9 TB/s of it; 32 of up to 4096, 4 key
+// heads, up to 5 tokens, 44 us, 3.1 TB/s (35 the shares, 8 stages each, 5 the joining); one of 1500 keys 11 us, two launches
 // of dependent reads.  Prompts are bound by the vector and matrix units together, which hardly overlap here (43 % and 42 %
-// busy): 2 chunks of 2048 tokens after 4096, 28 heads on 4, take 320 us, 940 TFLOP/s, batches of 16 of them 1027.  So the
+// busy): 2 chunks of 2048 tokens after 4096, 28 heads on 4, take 318 us, 945 TFLOP/s, batches of 16 of them 1026; 4 of
+// heads of 64, 16 on 16, 222 us, 774 (vector units 52 %, matrix units 34 %); 4 of heads of 256, 8 on 1, 395 us, 870.  So the
 // weights' exponentials, sums and roundings are nearly all that is left of the vector instructions in a stage, and
 // scores a stage ahead of the sums, their instructions woven into the weights', are slower for the registers they need.
 #include <algorithm>
@@ -584,10 +585,12 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void tiles_kernel(Paged P
     tile = u - min(max(P.cu_q[b], 0), P.T) * G / X::TM - b;
     if (tile < 0) return;  // before the first sequence
   } else if (a.bundle == 0) {
-    // Many units that all run at once: runs of 16 that follow one another go to one die, so that the keys are shared and chunks of many
-    // tiles spread over the dies; every other round of the dies is reversed, for a unit's tiles come the longest first
-    // (7 chunks of up to 77 tokens, a window of 300, 5 key heads: 8.2 us; with a unit a die 9.2, with an eighth of them all
-    // a die 9.9).
+    // Many units that all run at once: runs of 16 that follow one another go to one die, so that the keys are shared and
+    // chunks of many tiles spread over the dies; every other round of the dies is reversed, for a unit's tiles come the
+    // longest first (7 chunks of up to 77 tokens, a window of 300, 5 key heads: 8.2 us; with a unit a die 9.2, with an
+    // eighth of them all a die 9.9).  Against bundles as below it gains where tiles differ and hardly matters for one a unit
+    // (that case 9.4 us and 9.9, 64 single tokens 12.0 and 11.9, 12 ragged chunks of 40 17.8 and 17.7); 20 chunks of 30, all
+    // alike, it costs 32.7 us for 28.9.
     constexpr uint32_t kRun = 16;
     const uint32_t round = blockIdx.x / (8 * kRun), die = blockIdx.x % 8;
     const uint32_t at = (round * 8 + (round & 1 ? 7 - die : die)) * kRun + blockIdx.x / 8 % kRun;
@@ -887,17 +890,21 @@ int check(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_a
 //  - Up to 64 rows a sequence and key head: one tile of 32 or 64, and equal shares of the stages, two workgroups a compute
 //    unit, or fewer where there are fewer stages.
 //  - More rows: tiles of 128; where they are fewer than 3/4 of the workgroups that run at once the keys are split, into
-//    ranges of at least 512 (a chunk after a cache, 6144 keys together, 28 heads on 4 of 128: of 1280 tokens 148 us split
-//    and 160 whole, of 2048, 7/8 of the workgroups, 202 and 175).
-//    Where sequences times the tiles of the longest chunk exceed a launch, workgroups are numbered by the rows there are.
+//    ranges of 512 or more, made alike, so of 384 at least (a chunk after a cache, 6144 keys together, 28 heads on 4 of
+//    128: of 1280 tokens 148 us split and 160 whole, of 2048, 7/8 of the workgroups, 202 and 175).  Where sequences times
+//    the tiles of the longest chunk exceed a launch, workgroups are numbered by the rows there are (5000 chunks of up to 7
+//    tokens and one of 700, 16 heads on 1 of 64: 209 us).
 //  - Few keys, where tiles of 32 run all at once: those, a workgroup each for all its keys.  Four waves share a tile's
 //    keys, and nothing needs joining.  Up to 64 rows that saves the joining launch and costs the keys in turn: a token of 28
 //    heads on 4 of 128 after 256 keys takes 7.0 us so and 10.2 shared, after 512 9.4 and 10.6, after 1024 14.6 and 10.4;
 //    where the tiles fill the chip shares only add parts (64 tokens, 32 heads on 8, 1 to 2048 keys: 48 us and 59; 32
-//    chunks of 8: 30 and 42).  Heads of 256 have one workgroup a compute unit, and are slower so sooner.  Of more rows: 7
-//    chunks of up to 77 tokens under a window of 300, 5 key heads of 64, 8.5 us, and 14.6 with tiles of 128.  Over many
-//    keys they would be read too often: 14 times for 4 chunks of 64 tokens after 8192 with 7 heads a key head, that tiles of
-//    128, split, take 61 us for.
+//    chunks of 8: 30 and 42).  Where they fill half of it or more: 40 tokens of 28 heads on 4, 512 keys 13.1 us and 21.7,
+//    1024 19.7 and 25.9, 1536 27.3 and 30.9; of 60, 1024 24.3 and 31.4.  Heads of 256 have one workgroup a compute unit and
+//    are slower so sooner: a token of 8 heads on 1, 256 keys 10.9 us and 12.3, 384 12.9 and 13.0, 512 15.5 and 13.0; 40 of
+//    them, 384 15.1 and 14.7 (200 of them 20.9 and 43.6, and still faster so at 640).  Of more rows, against tiles of 128: 7
+//    chunks of up to 77 tokens, 5 key heads of 64, under a window of 300 9.3 us and 15.6, of 900 13.8 and 18.9; after 1024
+//    keys, all seen, 15.7 and 20.4, 2048 25.8 and 24.1; 4 chunks of 100, 28 heads on 4, 1024 22.6 and 28.9, 2048 36.5 and
+//    34.4; 2 of 128 with heads of 256, 1024 28.8 and 33.3, 2048 47.6 and 36.3.
 constexpr int kComputeUnits = 256;
 constexpr int64_t kMostBlocks = (int64_t)1 << 23;  // of a launch: below 2^32 threads
 struct Shape {
@@ -905,7 +912,7 @@ struct Shape {
   int64_t tiles, blocks;
   bool shares, join, packed;
   int64_t at_once;  // workgroups that run side by side (many rows)
-  int64_t parts;  // of a row, at most but for one or two
+  int64_t parts;  // of a row, on average over the units (a long sequence among short ones has more)
   size_t slots;   // of parts
 };
 Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_attend_args* g) {

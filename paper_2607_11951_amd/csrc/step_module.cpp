@@ -138,7 +138,8 @@ void no_gradient(std::initializer_list<const at::Tensor*> tensors) {
   const bool back = c10::GradMode::is_enabled(), forward = c10::AutogradState::get_tls_state().get_fw_grad_mode();
   for (const at::Tensor* t : tensors)
     if (t && ((back && t->requires_grad()) || (forward && t->_fw_grad(0).defined())))
-      throw Refused(PyExc_RuntimeError, "there are no gradients of this call: detach its tensors, or call it under torch.no_grad()");
+      throw Refused(PyExc_RuntimeError,
+                    "there are no gradients of this call: detach its tensors, or call it under torch.no_grad()");
 }
 // What a call has written in place, for torch to know.
 void written(std::initializer_list<const at::Tensor*> tensors) {

@@ -1,17 +1,19 @@
 // verify.hip -- grid_verify: drafted tokens against the target's masked distribution (gfx950).
 //
-// Two launches.  The first goes over the rows once: a workgroup takes a piece (some thousand tokens) of a row after the
-// other, with the noise of these tokens in registers, and leaves of each the largest allowed logit m, z = sum exp((l - m) / T), and the best of
-// the race exp((l - m) / T) / noise: an argmax that needs no normaliser and no order.  Logits are read only where the
-// mask allows one of a thread's 8 tokens.  The second joins a sequence's rows and finds the first refused draft.  Where
+// Two launches.  The first goes over the rows once: a workgroup takes a piece (some thousand tokens) of a row and leaves the
+// largest allowed logit m, z = sum exp((l - m) / T), and the best of the race exp((l - m) / T) / noise: an argmax that needs
+// no normaliser and no order.  Large batches have workgroups that take the piece of several rows of a sequence, one after
+// the other, with the noise of these tokens in registers.  Logits are read only where the mask allows one of a thread's 8
+// tokens.  The second joins a sequence's rows and finds the first refused draft.  Where
 // drafts come without probabilities, what is left of p after a refusal is p without the draft, so the first pass has
 // raced it already.  Otherwise max(p - q, 0) of that one row is raced by several workgroups, whose best meet in an integer
 // maximum (score bits, then the complement of the index: the lowest index on ties, whatever the order); the last of them
 // writes the sequence's outputs.
 //
-// Bound by latency more than by bytes: 32 sequences of up to 4 drafts, 151936 tokens in bf16, take 19.6 us (the first
-// launch 15.8, the second 4.6) for 52 MB of rows, masks and noise, of which the masked part is not read; 64 of up to 7, 50257
-// in float32, with the drafter's probabilities, 26.5 us (16.6 and 10.2, the race's atomics in turn among the latter).
+// Bound by latency more than by bytes: 32 sequences of up to 4 drafts, 151936 tokens in bf16, take 19.5 us (the first
+// launch 16.3, the second 4.5) for 52 MB of rows, masks and noise, of which the masked part is not read; 64 of up to 7, 50257
+// in float32, with the drafter's probabilities, 26.4 us (16.8 and 10.4, the race's atomics in turn among the latter).  The
+// former have one row a workgroup, the latter one or two: every chain of lengths, mask, logits and join begins anew.
 #include <algorithm>
 #include <string>
 #include <type_traits>
@@ -120,7 +122,7 @@ __device__ inline Row join_lanes(Row r, float c, bool greedy) {
   return {m, sum_across(r.z * f), best, idx};
 }
 
-// A workgroup takes a piece of the rows of one sequence that are in one group.
+// A workgroup takes a piece of the rows of one sequence that are in one group (one row, or several).
 enum class Rows { kAll, kMasked, kShort };  // all tokens allowed, mask rows, fewer than 8 tokens (masked or not)
 
 template <typename T, bool GREEDY, Rows ROWS>
@@ -402,8 +404,9 @@ __global__ __launch_bounds__(kThreads) void pick_kernel(VerifyArgs a) {
   if (tid == 0) a.accepted[b] = at;
 }
 
-// The launch.  A workgroup goes over rows of a sequence with its piece of the noise; the rows are dealt to so many groups
-// that there are about 4096 workgroups.  The residual's race is cut into about 1024 workgroups, none of less than a step.
+// The launch.  A sequence's rows are dealt to so many groups that there are about 4096 workgroups, or one for each row
+// (4096 was the best of 600 to 8192 for the batches above: fewer read the noise less often, and leave too few to run).  The
+// residual's race is cut into about 1024 workgroups, none of less than a step (the best of 512 to 4096).
 void plan(VerifyArgs& a, int steps) {
   a.pieces = (int32_t)(((int64_t)a.V + steps * kPiece - 1) / (steps * kPiece));
   const int64_t all = (int64_t)a.B * a.pieces;
