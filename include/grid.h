@@ -724,6 +724,195 @@ int grid_verify(const grid_verify_args* args, void* stream);
 /* 0 on bad sizes. */
 size_t grid_verify_workspace_bytes(int32_t B, int32_t K, int32_t V);
 
+/* ---------------------------------------------------------- trees of drafts */
+/* Where a grammar leaves a few continuations open a step drafts several at
+ * once: the chunk of a sequence is a tree of nodes, a node after its parent.
+ * parent[t] is the place in the chunk (0 ..) of the parent of the chunk's token
+ * t, -1 (or anything that is not below t's own place) where it has none.  A
+ * node's depth is the number of its ancestors; its position in the text is the
+ * number of cached tokens before the chunk and its depth. */
+
+/* What grid_attend_tree and grid_kv_append_tree are given of the trees, once a
+ * step: bit j of the words of token t (masks[t * stride_words + j / 32] >> j %
+ * 32) says that place j of t's chunk is t or an ancestor of t; depth[t] as
+ * above.  Bits past the chunk are 0.  Rows of sequences whose chunk is not in
+ * order, or longer than max_q, are zero bits and depth 0; rows of tokens that
+ * belong to no sequence are left as they are.  stride_words >= ceil(max_q /
+ * 32); n_tokens, n_seqs and cu_q as in grid_chunks. */
+typedef struct {
+  int32_t n_seqs;
+  int32_t n_tokens;
+  const int32_t* cu_q;     /* device [n_seqs + 1] */
+  const int32_t* parent;   /* device [n_tokens] */
+  int32_t max_q;           /* 1 .. 1024 */
+  int64_t stride_words;
+  uint32_t* masks;         /* device [n_tokens][stride_words] */
+  int32_t* depth;          /* device [n_tokens] */
+} grid_tree_args;
+int grid_tree_masks(const grid_tree_args* args, void* stream);
+
+/* grid_kv_append for trees: keys and queries are rotated by the position first
+ * + depth[t] (first: the cached tokens before the chunk), and lie at first +
+ * their place in the chunk.  A token of negative depth, or whose position has
+ * no row of cos and sin, is left out; so is, in a bad status, its sequence. */
+int grid_kv_append_tree(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_append_args* args,
+                        const int32_t* depth, void* stream);
+
+/* grid_attend for trees.  Token t sees the cached tokens before its chunk
+ * (with a window w > 0 of these the positions s > first + depth[t] - w), and of
+ * its chunk the places j whose bit is set in masks[t * stride_words + j / 32]:
+ * as grid_tree_masks writes them, or any others.  The rest is as there (the
+ * calls have workspaces of their own); a row that sees nothing is 0, its lse
+ * -inf.  With a window depth is not NULL, and a depth counts as at least 0 and
+ * less than the chunk. */
+typedef struct {
+  const uint32_t* masks;   /* device [n_tokens][stride_words], >= ceil(min(max_q, n_tokens) / 32) words each */
+  int64_t stride_words;
+  const int32_t* depth;    /* device [n_tokens], or NULL without a window */
+} grid_tree;
+int grid_attend_tree(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_attend_args* args,
+                     const grid_tree* tree, void* stream);
+size_t grid_attend_tree_workspace_bytes(const grid_paged_cache* cache, const grid_chunks* chunks,
+                                        const grid_attend_args* args);
+
+/* The branch of each tree that the target's tokens follow.  From place
+ * start[b] on (0 without start; its ancestors and itself are on the branch), as
+ * long as some child of the branch's last node c is the token sampled[c]: the
+ * first such child is the next.  Then length[b] nodes are on the branch,
+ * path[b * path_stride + i], i < length[b], are their places in the chunk, in
+ * order, -1 after them up to max_q; next[b] = sampled of the last.  With a
+ * cache the branch's rows are moved together, in every layer: what the cache
+ * holds at first + path[i] comes to first + i, so that first + length[b] tokens
+ * are cached.  What lies after them is left as it is.  Layer l's pages begin l
+ * * k_layer_stride (l * v_layer_stride) elements after the cache's.
+ * Of a bad sequence, an empty chunk, one longer than max_q, and a start that is
+ * not a place in the chunk, length is 0 and next -1, and nothing is moved; nor
+ * is a row whose page, or that of its place, is not in the cache.  No page may be
+ * in two sequences' chunks. */
+typedef struct {
+  const int32_t* tokens;       /* device [n_tokens]: the drafted tokens */
+  const int32_t* parent;       /* device [n_tokens] */
+  const int32_t* sampled;      /* device [n_tokens]: the target's token after each node, -1: none */
+  const int32_t* start;        /* device [n_seqs], or NULL */
+  int32_t max_q;               /* 1 .. 1024: bounds the chunks */
+  int32_t n_layers;            /* 1 .. 1024; 0: no cache, nothing is moved (of cache only the sizes are read) */
+  int64_t k_layer_stride;      /* in elements, multiples of 8 */
+  int64_t v_layer_stride;
+  int32_t* path;               /* device [n_seqs][path_stride] */
+  int64_t path_stride;         /* >= max_q */
+  int32_t* length;             /* device [n_seqs] */
+  int32_t* next;               /* device [n_seqs] */
+} grid_commit_args;
+int grid_commit_tree(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_commit_args* args, void* stream);
+
+/* --------------------------------------------------------- pages of a cache */
+/* Copies pages: of pair i the first rows[i] rows (all without rows; clamped to
+ * 0 .. page_size) of page src[i] to page dst[i], keys and values, in every
+ * layer (layer strides as in grid_commit_args).  Pairs with an id that is not
+ * in 0 .. n_pages - 1 are left out (-1: none).  No page that is written may be
+ * in another pair; a pair of one page twice does nothing. */
+typedef struct {
+  const int32_t* src;          /* device [n] */
+  const int32_t* dst;          /* device [n] */
+  const int32_t* rows;         /* device [n], or NULL */
+  int32_t n;                   /* 0 .. 2^20 */
+  int32_t n_layers;            /* 1 .. 1024 */
+  int64_t k_layer_stride;
+  int64_t v_layer_stride;
+} grid_copy_args;
+int grid_kv_copy(const grid_paged_cache* cache, const grid_copy_args* args, void* stream);
+
+/* The pages of the next step's rows.  Row b goes on from row parent[b] of the
+ * table (any number of rows from one; -1: from nothing) with its first keep[b]
+ * tokens, and gets room for room[b] tokens (keep[b], where that is more).  So a
+ * row that goes on by itself grows or gives pages back, a row that others go on
+ * from is forked, and what nobody goes on from is free again.
+ *
+ * refs[p] counts who holds page p: every row of the table that has it among its
+ * held[r] first entries, and whoever else the caller counts.  The call takes the
+ * table's rows out and puts the new rows in.  Row b keeps the first
+ * kept = ceil(keep / page_size) pages of its parent.  A row that writes into the
+ * last of them (room > keep, keep not a multiple of page_size) has it for itself:
+ * where all other holders are rows that write too, the lowest of these rows keeps
+ * it; the others get a page of their own in its place and copies says so:
+ * copies[b] = the page, copies[n_rows + b] = its copy, copies[2 * n_rows + b] =
+ * the keep % page_size rows to copy (-1, -1 and 0 where there is nothing to do),
+ * as grid_kv_copy takes them.  Free are the pages whose refs are 0 when the kept
+ * pages have been counted.  Rows get theirs in order, the lowest free page first,
+ * a row's copy before its new pages; from the first row on whose pages are more
+ * than are left no row gets any: such rows that need some keep what they have and
+ * have status GRID_ROW_OVERFLOW (a page that they write into may be shared).
+ * table_out: the pages, then -1; held_out their number.
+ * A row is bad (GRID_ROW_BAD_CONFIG; it holds nothing, its entries are -1, no
+ * copy) when parent is less than -1 or not below n_in, keep is negative or more
+ * than its parent's pages, room's pages are more than table_cols, or one of the
+ * entries it keeps is not a page.  held is clamped to 0 .. table_cols; entries
+ * that are not pages are not counted.  Without a parent keep is 0.
+ * refs_out may be refs.  No two of the other arrays may overlap. */
+typedef struct {
+  const int32_t* table;        /* device [n_in][table_stride] */
+  int64_t table_stride;        /* >= table_cols */
+  const int32_t* held;         /* device [n_in]: pages of each row */
+  int32_t n_in;                /* 1 .. 65535 */
+  int32_t n_rows;              /* 1 .. 65535 */
+  int32_t table_cols;          /* >= 1, table_cols * page_size < 2^31 */
+  int32_t n_pages;             /* 1 .. 2^26 */
+  int32_t page_size;           /* 1 .. 65536 */
+  const int32_t* parent;       /* device [n_rows] */
+  const int32_t* keep;         /* device [n_rows] */
+  const int32_t* room;         /* device [n_rows] */
+  const int32_t* refs;         /* device [n_pages] */
+  int32_t* table_out;          /* device [n_rows][table_out_stride] */
+  int64_t table_out_stride;    /* >= table_cols */
+  int32_t* held_out;           /* device [n_rows] */
+  int32_t* refs_out;           /* device [n_pages] */
+  int32_t* copies;             /* device [3][n_rows] */
+  int32_t* status;             /* device [n_rows] */
+  void* workspace;             /* device scratch, 16-byte aligned, grid_kv_fork_workspace_bytes; nothing is expected in it */
+  size_t workspace_bytes;
+} grid_fork_args;
+int grid_kv_fork(const grid_fork_args* args, void* stream);
+/* 0 on bad sizes. */
+size_t grid_kv_fork_workspace_bytes(int32_t n_rows, int32_t n_pages);
+
+/* ------------------------------------------------------------------- sample */
+/* One token of every row from its masked and filtered distribution, from given
+ * random numbers.  p = softmax(logits / temperature) over the tokens the mask row
+ * allows, in the order of the logits, the larger first, of equal ones the lower
+ * index first.  Of these are kept
+ *  - the first top_k (0 or less: all);
+ *  - of these the ones before which lies less than top_p of their mass (1 or
+ *    more: all);
+ *  - of these the ones whose p is at least min_p times the largest.
+ * The first is always kept.  The token is the kept one that makes p / noise the
+ * largest, the lowest such index: with noise drawn from Exp(1) it follows the
+ * kept ones' distribution.  logprobs[b] is the logarithm of its share of what is
+ * kept.  A temperature that is not above 0, or no noise, is greedy: the largest
+ * logit, its log p at temperature 1 among all allowed tokens, no filters.
+ * A row with no distribution (nothing allowed, or an allowed logit that is NaN or
+ * +inf) gives the token -1 and 0; so does one where noise that is not finite
+ * leaves no kept token a p / noise above 0 (noise is above 0 and finite; it is
+ * read at kept tokens only).  top_p or min_p that is NaN keeps all.
+ * Statistics are held in 32 bits or more. */
+typedef struct {
+  const void* logits;          /* device [B], rows of V */
+  int32_t dtype;               /* GRID_DTYPE_F32, _BF16 or _F16 */
+  int32_t B;                   /* 1 .. 2^20 */
+  int32_t V;                   /* 1 .. 2^30 - 2048 */
+  int64_t logits_stride;       /* in elements */
+  const uint32_t* mask;        /* device rows of the mask layout, or NULL: all allowed */
+  int64_t mask_stride;         /* in words */
+  const float* temperature;    /* device [B], or NULL: 1 */
+  const int32_t* top_k;        /* device [B], or NULL: all */
+  const float* top_p;
+  const float* min_p;
+  const float* noise;          /* device [B], rows of V, or NULL: greedy */
+  int64_t noise_stride;
+  int32_t* tokens;             /* device [B] */
+  float* logprobs;             /* device [B] */
+} grid_sample_args;
+int grid_sample(const grid_sample_args* args, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

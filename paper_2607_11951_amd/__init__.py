@@ -10,7 +10,7 @@ from .grid import (Grid, GridError, apply, mask_noalloc, from_workload, lib, CON
 
 def __getattr__(name):
     # the calls of step.py need torch, which compiling grammars does not
-    if name in ("attend", "kv_append", "verify"):
+    if name in ("attend", "attend_tree", "commit_tree", "kv_append", "kv_copy", "kv_fork", "sample", "tree_masks", "verify"):
         from . import step
         globals()[name] = getattr(step, name)
         return globals()[name]

@@ -13,7 +13,8 @@ OUT = PKG / "libgrid.so"
 MODULE = PKG / "_step.so"
 BUILD = PKG / "_build"
 HOST_SOURCES = ["grammar.cpp", "lexer.cpp", "parser.cpp", "artifacts.cpp", "advance.cpp", "complete.cpp", "capi.cpp"]
-HIP_SOURCES = ["kernels.hip", "paged.hip", "append.hip", "attend.hip", "verify.hip"]
+HIP_SOURCES = ["kernels.hip", "paged.hip", "append.hip", "attend.hip", "attend_tree.hip", "verify.hip", "sample.hip",
+               "tree.hip", "pages.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 HIP_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

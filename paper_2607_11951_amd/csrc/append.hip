@@ -27,6 +27,7 @@ struct AppendArgs {
   float eps, over;  // over = 1 / head_dim
   int32_t lanes;  // lanes of a head's vector
   int32_t base;   // the launch's first workgroup among all
+  const int32_t* depth;  // of trees: a token's position is the chunk's first and its depth
 };
 
 template <typename T>
@@ -38,7 +39,10 @@ struct alignas(16) Eight {
 // and a rotation.
 __device__ int status_of(const Paged& P, const AppendArgs& a, int b, bool ordered) {
   const Chunk c = chunk_of(P, b);
-  bool ok = ordered && c.ok && (!a.cos || c.kv <= a.n_positions || c.n == 0);
+  bool ok = ordered && c.ok && (!a.cos || a.depth || c.kv <= a.n_positions || c.n == 0);
+  if (ok && a.depth)
+    for (int t = c.first; t < c.first + c.n; ++t)
+      ok = ok && a.depth[t] >= 0 && (!a.cos || (int64_t)c.kv - c.n + a.depth[t] < a.n_positions);
   if (ok && c.n > 0) {
     const uint32_t from = P.page.quot((uint32_t)(c.kv - c.n)), to = P.page.quot((uint32_t)(c.kv - 1));
     for (uint32_t p = from; p <= to; ++p) ok = ok && P.in_cache(P.table[(int64_t)b * P.table_stride + p]);
@@ -88,13 +92,16 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Paged P, AppendArgs a)
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i)
     if (u_first + i * groups < vectors) ahead[i] = source(u_first + i * groups);
+  const int depth = a.depth ? a.depth[t] : -1;
   int b;
   const Chunk c = chunk_of_token(P, t, b);
+  if (a.depth && depth < 0) return;
   if (!c.ok || t < c.first || t >= c.first + c.n) return;
-  const int pos = c.kv - c.n + t - c.first;
+  const int place = c.kv - c.n + t - c.first;
+  const int64_t pos = depth < 0 ? place : (int64_t)c.kv - c.n + depth;
   if (TURN != Turn::kNone && pos >= a.n_positions) return;
   uint32_t row;
-  const int page = P.page_of(b, (uint32_t)pos, row);
+  const int page = P.page_of(b, (uint32_t)place, row);
   // the rotation of the lane's entries; in halves, hp lanes apart: the partner's lane and entries
   float cs[8], sn[8];
   const int hp = a.half / 8;
@@ -102,7 +109,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(Paged P, AppendArgs a)
   const int other = low ? lane + hp : lane - hp, oe = low ? e + a.half : e - a.half;
   if (TURN != Turn::kNone && turned) {
     constexpr int N = TURN == Turn::kPairs ? 4 : 8;
-    const int64_t at = (int64_t)pos * a.half + (TURN == Turn::kPairs ? e / 2 : low ? e : oe);
+    const int64_t at = pos * a.half + (TURN == Turn::kPairs ? e / 2 : low ? e : oe);
     __builtin_memcpy(cs, a.cos + at, N * 4);
     __builtin_memcpy(sn, a.sin + at, N * 4);
   }
@@ -184,14 +191,12 @@ void launch(const Paged& P, const AppendArgs& a, unsigned blocks, hipStream_t st
     norm ? go(append_kernel<T, Turn::kHalves, true>) : go(append_kernel<T, Turn::kHalves, false>);
 }
 
-}  // namespace
-
-extern "C" int grid_kv_append(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_append_args* args,
-                              void* stream) {
-  clear_error();
-  const int rc = check_paged("grid_kv_append", cache, chunks, true);
+// Either call: depth is not NULL in the trees'.
+int append(const std::string& call, const grid_paged_cache* cache, const grid_chunks* chunks, const grid_append_args* args,
+           const int32_t* depth, void* stream) {
+  const int rc = check_paged(call.c_str(), cache, chunks, true);
   if (rc != GRID_OK) return rc;
-  auto bad = [](const char* what) { return fail(GRID_E_ARG, std::string("grid_kv_append: ") + what); };
+  auto bad = [&](const char* what) { return fail(GRID_E_ARG, call + ": " + what); };
   if (!args) return bad("null argument");
   const grid_append_args& g = *args;
   const int D = cache->head_dim;
@@ -225,6 +230,7 @@ extern "C" int grid_kv_append(const grid_paged_cache* cache, const grid_chunks* 
   a.half = g.rot_dim / 2;
   a.interleaved = g.interleaved;
   a.eps = g.eps;
+  a.depth = depth;
   a.over = 1.f / (float)D;
   a.lanes = 1;
   while (a.lanes * 8 < D) a.lanes *= 2;
@@ -240,6 +246,21 @@ extern "C" int grid_kv_append(const grid_paged_cache* cache, const grid_chunks* 
       launch<f16_t>(P, a, n, (hipStream_t)stream);
   }
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return fail(GRID_E_HIP, std::string("grid_kv_append launch: ") + hipGetErrorString(e));
+  if (e != hipSuccess) return fail(GRID_E_HIP, call + " launch: " + hipGetErrorString(e));
   return GRID_OK;
+}
+
+}  // namespace
+
+extern "C" int grid_kv_append(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_append_args* args,
+                              void* stream) {
+  clear_error();
+  return append("grid_kv_append", cache, chunks, args, nullptr, stream);
+}
+
+extern "C" int grid_kv_append_tree(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_append_args* args,
+                                   const int32_t* depth, void* stream) {
+  clear_error();
+  if (!depth) return fail(GRID_E_ARG, "grid_kv_append_tree: no depths");
+  return append("grid_kv_append_tree", cache, chunks, args, depth, stream);
 }

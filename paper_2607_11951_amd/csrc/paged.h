@@ -52,11 +52,14 @@ struct Paged {
   __device__ bool in_cache(int id) const { return (uint32_t)id < (uint32_t)n_pages; }
 };
 
-// Checks a cache and chunks; the message names the call.
+// Checks a cache, or a cache and chunks; the message names the call.
+int check_cache(const char* call, const grid_paged_cache* c, bool pointers);
 int check_paged(const char* call, const grid_paged_cache* c, const grid_chunks* x, bool pointers);
 Paged make_paged(const grid_paged_cache* c, const grid_chunks* x);
 // Whether rows at these strides (elements of 16 bits, below 2^31) can be read 16 bytes at a time.
 bool rows_fit(const void* p, const int64_t* strides, int n);
+// Whether layers may lie so far apart.
+bool layers_fit(int layers, int64_t k_stride, int64_t v_stride);
 
 struct Chunk {
   int32_t first, n, kv;  // first token, new tokens, cached tokens with them

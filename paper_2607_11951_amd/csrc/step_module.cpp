@@ -13,6 +13,7 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cmath>
 #include <initializer_list>
 #include <stdexcept>
@@ -84,7 +85,15 @@ int32_t half_type(at::ScalarType t, const char* what) {
   throw Refused(PyExc_TypeError, what);
 }
 
-grid_paged_cache paged(const at::Tensor& k, const at::Tensor& v) {
+grid_paged_cache paged(const at::Tensor& k, const at::Tensor& v, int64_t* layers = nullptr) {
+  if (layers && k.dim() == 5) {
+    need(k.sizes() == v.sizes() && k.scalar_type() == v.scalar_type() && k.size(0) >= 1,
+         "pages: [layers, pages, page_size, heads, head_dim], keys and values alike");
+    layers[0] = k.size(0);
+    layers[1] = k.stride(0);
+    layers[2] = v.stride(0);
+    return paged(k.select(0, 0), v.select(0, 0));
+  }
   need(k.dim() == 4 && k.sizes() == v.sizes() && k.scalar_type() == v.scalar_type() && k.device() == v.device(),
        "pages: [pages, page_size, heads, head_dim], keys and values alike");
   grid_paged_cache c;
@@ -170,9 +179,9 @@ PyObject* guarded(Py_ssize_t n, Py_ssize_t want, F f) {
   return nullptr;
 }
 
-// k, v, k_pages, v_pages, block_table, kv_len, cu_q, q, q_out, cos, sin, interleaved, q_norm, k_norm, eps, status
+// k, v, k_pages, v_pages, block_table, kv_len, cu_q, q, q_out, cos, sin, interleaved, q_norm, k_norm, eps, status, depth
 PyObject* kv_append(PyObject*, PyObject* const* x, Py_ssize_t n) {
-  return guarded(n, 16, [&]() -> PyObject* {
+  return guarded(n, 17, [&]() -> PyObject* {
     const at::Tensor &k = tensor(x[0], "k"), &v = tensor(x[1], "v"), &k_pages = tensor(x[2], "k_pages");
     const at::Tensor& v_pages = tensor(x[3], "v_pages");
     const grid_paged_cache c = paged(k_pages, v_pages);
@@ -203,6 +212,8 @@ PyObject* kv_append(PyObject*, PyObject* const* x, Py_ssize_t n) {
     dense(q_norm, at::kFloat, {D}, dev, "q_norm");
     dense(k_norm, at::kFloat, {D}, dev, "k_norm");
     dense(status, at::kInt, {ch.n_seqs}, dev, "status");
+    const at::Tensor* depth = maybe(x[16], "depth");
+    dense(depth, at::kInt, {tokens}, dev, "depth");
     a.q_norm = ptr<float>(q_norm);
     a.k_norm = ptr<float>(k_norm);
     a.eps = real(x[14], "eps");
@@ -221,7 +232,11 @@ PyObject* kv_append(PyObject*, PyObject* const* x, Py_ssize_t n) {
       a.q_out = ptr(out);
       a.n_heads = small(q->size(1), "q");
     }
-    const int rc = grid_kv_append(&c, &ch, &a, stream);
+    int rc;
+    if (!depth)
+      rc = grid_kv_append(&c, &ch, &a, stream);
+    else
+      rc = tokens ? grid_kv_append_tree(&c, &ch, &a, ptr<int32_t>(depth), stream) : grid_kv_append(&c, &ch, &a, stream);
     if (rc != GRID_OK) return PyLong_FromLong(rc);
     written({&k_pages, &v_pages, q ? q_out : nullptr, status});
     PyObject* first = q ? given(x[8], out) : (Py_INCREF(Py_None), Py_None);
@@ -231,9 +246,9 @@ PyObject* kv_append(PyObject*, PyObject* const* x, Py_ssize_t n) {
   });
 }
 
-// q, k_pages, v_pages, block_table, kv_len, cu_q, max_q, max_kv, scale, window, out, lse, workspace
-PyObject* attend(PyObject*, PyObject* const* x, Py_ssize_t n) {
-  return guarded(n, 13, [&]() -> PyObject* {
+// q, k_pages, v_pages, block_table, kv_len, cu_q, max_q, max_kv, scale, window, out, lse, workspace; trees: tree, depth
+PyObject* attend_call(PyObject* const* x, Py_ssize_t n, bool trees) {
+  return guarded(n, trees ? 15 : 13, [&]() -> PyObject* {
     const at::Tensor &q = tensor(x[0], "q"), &k_pages = tensor(x[1], "k_pages"), &v_pages = tensor(x[2], "v_pages");
     const grid_paged_cache c = paged(k_pages, v_pages);
     const at::Device dev = k_pages.device();
@@ -248,6 +263,17 @@ PyObject* attend(PyObject*, PyObject* const* x, Py_ssize_t n) {
     a.max_kv = whole(x[7], "max_kv");
     a.scale = x[8] == Py_None ? 1.0f / std::sqrt((float)D) : real(x[8], "scale");
     a.window = whole(x[9], "window");
+    const at::Tensor *masks = trees ? &tensor(x[13], "tree") : nullptr, *depth = trees ? maybe(x[14], "depth") : nullptr;
+    grid_tree tree = {};
+    if (trees) {
+      need(masks->dim() == 2 && masks->scalar_type() == at::kInt && masks->device() == dev && masks->size(0) == tokens &&
+               masks->size(1) >= (std::min<int64_t>(a.max_q, tokens) + 31) / 32 && masks->stride(1) == 1,
+           "tree: an int32 tensor [tokens, words of max_q bits or more] with dense rows");
+      dense(depth, at::kInt, {tokens}, dev, "depth");
+      tree.masks = ptr<uint32_t>(masks);
+      tree.stride_words = tokens > 1 ? masks->stride(0) : masks->size(1);
+      tree.depth = ptr<int32_t>(depth);
+    }
     const at::Tensor* given_lse = maybe(x[11], "lse");
     dense(given_lse, at::kFloat, {tokens, q.size(1)}, dev, "lse");
     const at::Tensor *given_out = maybe(x[10], "out"), *given_work = maybe(x[12], "workspace");
@@ -262,11 +288,13 @@ PyObject* attend(PyObject*, PyObject* const* x, Py_ssize_t n) {
     a.lse = ptr<float>(lse);
     const at::Tensor work =
         given_work ? *given_work
-                   : at::empty({(int64_t)grid_attend_workspace_bytes(&c, &ch, &a)}, q.options().dtype(at::kByte));
+                   : at::empty({(int64_t)(trees ? grid_attend_tree_workspace_bytes(&c, &ch, &a)
+                                                : grid_attend_workspace_bytes(&c, &ch, &a))},
+                               q.options().dtype(at::kByte));
     need(work.device() == dev && work.is_contiguous(), "workspace: a contiguous tensor on the cache's device");
     a.workspace = ptr(work);
     a.workspace_bytes = work.nbytes();
-    const int rc = grid_attend(&c, &ch, &a, stream);
+    const int rc = trees ? grid_attend_tree(&c, &ch, &a, &tree, stream) : grid_attend(&c, &ch, &a, stream);
     if (rc != GRID_OK) return PyLong_FromLong(rc);
     written({given_out, given_lse, given_work});
     PyObject *o = given(x[10], out), *l = given(x[11], lse), *both = PyTuple_Pack(2, o, l);
@@ -275,6 +303,8 @@ PyObject* attend(PyObject*, PyObject* const* x, Py_ssize_t n) {
     return both;
   });
 }
+PyObject* attend(PyObject*, PyObject* const* x, Py_ssize_t n) { return attend_call(x, n, false); }
+PyObject* attend_tree(PyObject*, PyObject* const* x, Py_ssize_t n) { return attend_call(x, n, true); }
 
 // logits, draft, draft_len, mask, draft_probs, uniform, noise, temperature, tokens, accepted, logprobs, workspace
 PyObject* verify(PyObject*, PyObject* const* x, Py_ssize_t n) {
@@ -357,9 +387,274 @@ PyObject* verify(PyObject*, PyObject* const* x, Py_ssize_t n) {
   });
 }
 
+// parent, cu_q, max_q, masks, depth
+PyObject* tree_masks(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  return guarded(n, 5, [&]() -> PyObject* {
+    const at::Tensor &parent = tensor(x[0], "parent"), &cu_q = tensor(x[1], "cu_q");
+    const at::Device dev = parent.device();
+    need(parent.dim() == 1, "parent: [tokens]");
+    need(cu_q.dim() == 1 && cu_q.size(0) >= 2, "cu_q: [B + 1]");
+    dense(&parent, at::kInt, parent.sizes(), dev, "parent");
+    dense(&cu_q, at::kInt, cu_q.sizes(), dev, "cu_q");
+    grid_tree_args a = {};
+    a.n_tokens = small(parent.size(0), "parent");
+    a.n_seqs = small(cu_q.size(0) - 1, "cu_q");
+    a.max_q = whole(x[2], "max_q");
+    need(a.max_q >= 1, "max_q");
+    const int64_t T = parent.size(0), words = ((int64_t)a.max_q + 31) / 32;
+    const at::Tensor *m = maybe(x[3], "masks"), *d = maybe(x[4], "depth");
+    if (m)
+      need(m->dim() == 2 && m->scalar_type() == at::kInt && m->device() == dev && m->size(0) == T && m->size(1) >= words &&
+               m->stride(1) == 1,
+           "masks: an int32 tensor [tokens, words of max_q bits or more] with dense rows");
+    dense(d, at::kInt, {T}, dev, "depth");
+    void* stream = stream_of(dev);
+    const c10::DeviceGuard guard(dev);
+    const at::Tensor masks = m ? *m : at::empty({T, words}, parent.options());
+    const at::Tensor depth = d ? *d : at::empty({T}, parent.options());
+    a.cu_q = ptr<int32_t>(cu_q);
+    a.parent = ptr<int32_t>(parent);
+    a.masks = ptr<uint32_t>(masks);
+    a.stride_words = T > 1 ? masks.stride(0) : masks.size(1);
+    a.depth = ptr<int32_t>(depth);
+    const int rc = grid_tree_masks(&a, stream);
+    if (rc != GRID_OK) return PyLong_FromLong(rc);
+    written({m, d});
+    PyObject *p = given(x[3], masks), *q = given(x[4], depth), *both = PyTuple_Pack(2, p, q);
+    Py_DECREF(p);
+    Py_DECREF(q);
+    return both;
+  });
+}
+
+// k_pages, v_pages, block_table, kv_len, cu_q, tokens, parent, sampled, max_q, start, path, length, next
+PyObject* commit_tree(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  return guarded(n, 13, [&]() -> PyObject* {
+    const at::Tensor &cu_q = tensor(x[4], "cu_q"), &tokens = tensor(x[5], "tokens"), &parent = tensor(x[6], "parent");
+    const at::Tensor& sampled = tensor(x[7], "sampled");
+    const at::Device dev = cu_q.device();
+    need(cu_q.dim() == 1 && cu_q.size(0) >= 2, "cu_q: [B + 1]");
+    need(tokens.dim() == 1, "tokens: [tokens]");
+    const int64_t B = cu_q.size(0) - 1, T = tokens.size(0);
+    const at::Tensor *k_pages = maybe(x[0], "k_pages"), *v_pages = maybe(x[1], "v_pages"), *start = maybe(x[9], "start");
+    dense(&cu_q, at::kInt, {B + 1}, dev, "cu_q");
+    dense(&tokens, at::kInt, {T}, dev, "tokens");
+    dense(&parent, at::kInt, {T}, dev, "parent");
+    dense(&sampled, at::kInt, {T}, dev, "sampled");
+    dense(start, at::kInt, {B}, dev, "start");
+    need(!k_pages == !v_pages, "k_pages and v_pages come together");
+    grid_paged_cache c = {};
+    grid_chunks ch = {};
+    grid_commit_args a = {};
+    if (k_pages) {
+      int64_t layers[3] = {1, 0, 0};
+      c = paged(*k_pages, *v_pages, layers);
+      need(k_pages->device() == dev, "the cache is on the device of cu_q");
+      ch = chunks(T, tensor(x[2], "block_table"), tensor(x[3], "kv_len"), cu_q, dev);
+      a.n_layers = small(layers[0], "layers");
+      a.k_layer_stride = layers[1];
+      a.v_layer_stride = layers[2];
+    } else {
+      ch.n_seqs = small(B, "cu_q");
+      ch.n_tokens = small(T, "tokens");
+      ch.cu_q = ptr<int32_t>(cu_q);
+    }
+    a.max_q = whole(x[8], "max_q");
+    need(a.max_q >= 1, "max_q");
+    const at::Tensor *p = maybe(x[10], "path"), *l = maybe(x[11], "length"), *f = maybe(x[12], "next");
+    dense(p, at::kInt, {B, a.max_q}, dev, "path");
+    dense(l, at::kInt, {B}, dev, "length");
+    dense(f, at::kInt, {B}, dev, "next");
+    no_gradient({k_pages, v_pages});
+    void* stream = stream_of(dev);
+    const c10::DeviceGuard guard(dev);
+    const at::Tensor path = p ? *p : at::empty({B, a.max_q}, cu_q.options());
+    const at::Tensor length = l ? *l : at::empty({B}, cu_q.options()), next = f ? *f : at::empty({B}, cu_q.options());
+    a.tokens = ptr<int32_t>(tokens);
+    a.parent = ptr<int32_t>(parent);
+    a.sampled = ptr<int32_t>(sampled);
+    a.start = ptr<int32_t>(start);
+    a.path = ptr<int32_t>(path);
+    a.path_stride = a.max_q;
+    a.length = ptr<int32_t>(length);
+    a.next = ptr<int32_t>(next);
+    const int rc = grid_commit_tree(k_pages ? &c : nullptr, &ch, &a, stream);
+    if (rc != GRID_OK) return PyLong_FromLong(rc);
+    written({k_pages, v_pages, p, l, f});
+    PyObject *r0 = given(x[10], path), *r1 = given(x[11], length), *r2 = given(x[12], next), *all = PyTuple_Pack(3, r0, r1, r2);
+    Py_DECREF(r0);
+    Py_DECREF(r1);
+    Py_DECREF(r2);
+    return all;
+  });
+}
+
+// k_pages, v_pages, src, dst, rows
+PyObject* kv_copy(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  return guarded(n, 5, [&]() -> PyObject* {
+    const at::Tensor &k_pages = tensor(x[0], "k_pages"), &v_pages = tensor(x[1], "v_pages");
+    int64_t layers[3] = {1, 0, 0};
+    const grid_paged_cache c = paged(k_pages, v_pages, layers);
+    const at::Device dev = k_pages.device();
+    const at::Tensor &src = tensor(x[2], "src"), &dst = tensor(x[3], "dst"), *rows = maybe(x[4], "rows");
+    need(src.dim() == 1, "src: [pairs]");
+    dense(&src, at::kInt, src.sizes(), dev, "src");
+    dense(&dst, at::kInt, src.sizes(), dev, "dst");
+    dense(rows, at::kInt, src.sizes(), dev, "rows");
+    no_gradient({&k_pages, &v_pages});
+    void* stream = stream_of(dev);
+    const c10::DeviceGuard guard(dev);
+    grid_copy_args a = {};
+    a.src = ptr<int32_t>(src);
+    a.dst = ptr<int32_t>(dst);
+    a.rows = ptr<int32_t>(rows);
+    a.n = small(src.size(0), "pairs");
+    a.n_layers = small(layers[0], "layers");
+    a.k_layer_stride = layers[1];
+    a.v_layer_stride = layers[2];
+    const int rc = grid_kv_copy(&c, &a, stream);
+    if (rc != GRID_OK) return PyLong_FromLong(rc);
+    written({&k_pages, &v_pages});
+    Py_RETURN_NONE;
+  });
+}
+
+// block_table, held, parent, keep, room, refs, page_size, table_out, held_out, refs_out, copies, status, workspace
+PyObject* kv_fork(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  return guarded(n, 13, [&]() -> PyObject* {
+    const at::Tensor &table = tensor(x[0], "block_table"), &held = tensor(x[1], "held"), &parent = tensor(x[2], "parent");
+    const at::Tensor &keep = tensor(x[3], "keep"), &room = tensor(x[4], "room"), &refs = tensor(x[5], "refs");
+    const at::Device dev = table.device();
+    need(table.dim() == 2 && table.scalar_type() == at::kInt && table.stride(1) == 1,
+         "block_table: an int32 tensor [rows, pages] with dense rows");
+    need(parent.dim() == 1 && refs.dim() == 1, "parent: [rows]; refs: [pages]");
+    const int64_t in = table.size(0), R = parent.size(0), cols = table.size(1);
+    dense(&held, at::kInt, {in}, dev, "held");
+    dense(&parent, at::kInt, {R}, dev, "parent");
+    dense(&keep, at::kInt, {R}, dev, "keep");
+    dense(&room, at::kInt, {R}, dev, "room");
+    dense(&refs, at::kInt, refs.sizes(), dev, "refs");
+    const at::Tensor *t = maybe(x[7], "table_out"), *h = maybe(x[8], "held_out"), *r = maybe(x[9], "refs_out");
+    const at::Tensor *c = maybe(x[10], "copies"), *s = maybe(x[11], "status"), *given_work = maybe(x[12], "workspace");
+    if (t)
+      need(t->dim() == 2 && t->scalar_type() == at::kInt && t->device() == dev && t->size(0) == R && t->size(1) == cols &&
+               t->stride(1) == 1,
+           "table_out: an int32 tensor [rows, pages] with dense rows");
+    dense(h, at::kInt, {R}, dev, "held_out");
+    dense(r, at::kInt, refs.sizes(), dev, "refs_out");
+    dense(c, at::kInt, {3, R}, dev, "copies");
+    dense(s, at::kInt, {R}, dev, "status");
+    grid_fork_args a = {};
+    a.n_in = small(in, "block_table");
+    a.n_rows = small(R, "parent");
+    a.table_cols = small(cols, "block_table");
+    a.n_pages = small(refs.size(0), "refs");
+    a.page_size = whole(x[6], "page_size");
+    void* stream = stream_of(dev);
+    const c10::DeviceGuard guard(dev);
+    const auto ints = table.options();
+    const at::Tensor out = t ? *t : at::empty({R, cols}, ints), held_out = h ? *h : at::empty({R}, ints);
+    const at::Tensor refs_out = r ? *r : at::empty_like(refs), copies = c ? *c : at::empty({3, R}, ints);
+    const at::Tensor status = s ? *s : at::empty({R}, ints);
+    const at::Tensor work =
+        given_work ? *given_work
+                   : at::empty({(int64_t)grid_kv_fork_workspace_bytes(a.n_rows, a.n_pages)}, ints.dtype(at::kByte));
+    need(work.device() == dev && work.is_contiguous(), "workspace: a contiguous tensor on the table's device");
+    a.table = ptr<int32_t>(table);
+    a.table_stride = in > 1 ? table.stride(0) : cols;
+    a.held = ptr<int32_t>(held);
+    a.parent = ptr<int32_t>(parent);
+    a.keep = ptr<int32_t>(keep);
+    a.room = ptr<int32_t>(room);
+    a.refs = ptr<int32_t>(refs);
+    a.table_out = ptr<int32_t>(out);
+    a.table_out_stride = R > 1 ? out.stride(0) : cols;
+    a.held_out = ptr<int32_t>(held_out);
+    a.refs_out = ptr<int32_t>(refs_out);
+    a.copies = ptr<int32_t>(copies);
+    a.status = ptr<int32_t>(status);
+    a.workspace = ptr(work);
+    a.workspace_bytes = work.nbytes();
+    const int rc = grid_kv_fork(&a, stream);
+    if (rc != GRID_OK) return PyLong_FromLong(rc);
+    written({t, h, r, c, s, given_work});
+    PyObject* all = PyTuple_New(5);
+    PyTuple_SET_ITEM(all, 0, given(x[7], out));
+    PyTuple_SET_ITEM(all, 1, given(x[8], held_out));
+    PyTuple_SET_ITEM(all, 2, given(x[9], refs_out));
+    PyTuple_SET_ITEM(all, 3, given(x[10], copies));
+    PyTuple_SET_ITEM(all, 4, given(x[11], status));
+    return all;
+  });
+}
+
+// logits, mask, temperature, top_k, top_p, min_p, noise, tokens, logprobs
+PyObject* sample(PyObject*, PyObject* const* x, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> PyObject* {
+    const at::Tensor& logits = tensor(x[0], "logits");
+    need(logits.dim() == 2 && logits.stride(1) == 1, "logits: [rows, V] with dense rows");
+    grid_sample_args a = {};
+    a.dtype = logits.scalar_type() == at::kFloat ? GRID_DTYPE_F32
+                                                 : half_type(logits.scalar_type(), "logits must be float32, bfloat16 or float16");
+    const int64_t B = logits.size(0), V = logits.size(1), words = (V + 31) / 32;
+    const at::Device dev = logits.device();
+    a.logits = ptr(logits);
+    a.B = small(B, "logits");
+    a.V = small(V, "logits");
+    a.logits_stride = logits.stride(0);
+    const at::Tensor *mask = maybe(x[1], "mask"), *temperature = maybe(x[2], "temperature"), *top_k = maybe(x[3], "top_k");
+    const at::Tensor *top_p = maybe(x[4], "top_p"), *min_p = maybe(x[5], "min_p"), *noise = maybe(x[6], "noise");
+    dense(temperature, at::kFloat, {B}, dev, "temperature");
+    dense(top_k, at::kInt, {B}, dev, "top_k");
+    dense(top_p, at::kFloat, {B}, dev, "top_p");
+    dense(min_p, at::kFloat, {B}, dev, "min_p");
+    if (mask) {
+      need(mask->dim() == 2 && mask->scalar_type() == at::kInt && mask->device() == dev && mask->size(0) == B &&
+               mask->size(1) >= words && mask->stride(1) == 1,
+           "mask: an int32 tensor [rows, words of V bits or more] with dense rows");
+      a.mask_stride = mask->stride(0);
+    }
+    if (noise) {
+      need(noise->dim() == 2 && noise->scalar_type() == at::kFloat && noise->device() == dev && noise->size(0) == B &&
+               noise->size(1) == V && noise->stride(1) == 1,
+           "noise: a float32 tensor [rows, V] with dense rows");
+      a.noise_stride = noise->stride(0);
+    }
+    const at::Tensor *t = maybe(x[7], "tokens"), *l = maybe(x[8], "logprobs");
+    dense(t, at::kInt, {B}, dev, "tokens");
+    dense(l, at::kFloat, {B}, dev, "logprobs");
+    no_gradient({&logits, temperature, top_p, min_p, noise, l});
+    void* stream = stream_of(dev);
+    const c10::DeviceGuard guard(dev);
+    const auto ints = logits.options().dtype(at::kInt);
+    const at::Tensor tokens = t ? *t : at::empty({B}, ints), logprobs = l ? *l : at::empty({B}, ints.dtype(at::kFloat));
+    a.mask = ptr<uint32_t>(mask);
+    a.temperature = ptr<float>(temperature);
+    a.top_k = ptr<int32_t>(top_k);
+    a.top_p = ptr<float>(top_p);
+    a.min_p = ptr<float>(min_p);
+    a.noise = ptr<float>(noise);
+    a.tokens = ptr<int32_t>(tokens);
+    a.logprobs = ptr<float>(logprobs);
+    const int rc = grid_sample(&a, stream);
+    if (rc != GRID_OK) return PyLong_FromLong(rc);
+    written({t, l});
+    PyObject *p = given(x[7], tokens), *q = given(x[8], logprobs), *both = PyTuple_Pack(2, p, q);
+    Py_DECREF(p);
+    Py_DECREF(q);
+    return both;
+  });
+}
+
 PyMethodDef methods[] = {{"kv_append", (PyCFunction)(void (*)(void))kv_append, METH_FASTCALL, nullptr},
                          {"attend", (PyCFunction)(void (*)(void))attend, METH_FASTCALL, nullptr},
                          {"verify", (PyCFunction)(void (*)(void))verify, METH_FASTCALL, nullptr},
+                         {"tree_masks", (PyCFunction)(void (*)(void))tree_masks, METH_FASTCALL, nullptr},
+                         {"attend_tree", (PyCFunction)(void (*)(void))attend_tree, METH_FASTCALL, nullptr},
+                         {"commit_tree", (PyCFunction)(void (*)(void))commit_tree, METH_FASTCALL, nullptr},
+                         {"kv_copy", (PyCFunction)(void (*)(void))kv_copy, METH_FASTCALL, nullptr},
+                         {"kv_fork", (PyCFunction)(void (*)(void))kv_fork, METH_FASTCALL, nullptr},
+                         {"sample", (PyCFunction)(void (*)(void))sample, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_step", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

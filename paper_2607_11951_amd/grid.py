@@ -48,7 +48,9 @@ EXPORTS = ["grid_compile", "grid_free", "grid_last_error", "grid_info", "grid_ad
            "grid_mask_noalloc_max_bytes", "grid_mask_noalloc", "grid_stack_hash", "grid_stack_hash_host",
            "grid_accept_inplace", "grid_ci_cache_bytes", "grid_ci_cache_clear", "grid_mask_warm",
            "grid_complete", "grid_forced_span", "grid_forced_span_workspace_bytes", "grid_kv_append", "grid_attend",
-           "grid_attend_workspace_bytes", "grid_verify", "grid_verify_workspace_bytes"]
+           "grid_attend_workspace_bytes", "grid_verify", "grid_verify_workspace_bytes", "grid_tree_masks",
+           "grid_kv_append_tree", "grid_attend_tree", "grid_attend_tree_workspace_bytes", "grid_commit_tree",
+           "grid_kv_copy", "grid_kv_fork", "grid_kv_fork_workspace_bytes", "grid_sample"]
 CI_LOOKUP, CI_INSERT, CI_FAMILY, CI_GENN = 1, 2, 4, 8
 PHASE_PROLOGUE, PHASE_WALK, PHASE_RESIDUE, PHASE_FINALIZE, PHASE_ALL = 1, 2, 4, 8, 15
 
@@ -131,6 +133,17 @@ def lib():
         L.grid_verify.argtypes = [vp, vp]
         L.grid_verify_workspace_bytes.argtypes = [i32, i32, i32]
         L.grid_verify_workspace_bytes.restype = sz
+        L.grid_tree_masks.argtypes = [vp, vp]
+        L.grid_kv_append_tree.argtypes = [vp, vp, vp, vp, vp]
+        L.grid_attend_tree.argtypes = [vp, vp, vp, vp, vp]
+        L.grid_attend_tree_workspace_bytes.argtypes = [vp, vp, vp]
+        L.grid_attend_tree_workspace_bytes.restype = sz
+        L.grid_commit_tree.argtypes = [vp, vp, vp, vp]
+        L.grid_kv_copy.argtypes = [vp, vp, vp]
+        L.grid_kv_fork.argtypes = [vp, vp]
+        L.grid_kv_fork_workspace_bytes.argtypes = [i32, i32]
+        L.grid_kv_fork_workspace_bytes.restype = sz
+        L.grid_sample.argtypes = [vp, vp]
         _lib = L
     return _lib
 

@@ -1,0 +1,274 @@
+"""grid_sample on the GPU against its definition in 64 bits.
+
+Tokens are decisions: they are equal unless two racers come within rounding, or a mass or weight comes within rounding of its
+filter (a relative 1e-5 here, for which the reference says whether it was that close; the inputs are such that none is).  A
+log probability is (l - m) / T - log z in 32 bits: off by at most 2^-22 (|l - m| / T + |log z| + 1) and a relative error of z,
+a sum of V terms of which a thread adds at most V / 1024 + 8 in a row and some twenty joins: below 2^-14.6 up to V = 600000.
+"""
+
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def G():
+    import paper_2607_11951_amd as pkg
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    pkg.lib()
+    return pkg
+
+
+def pack(bits):
+    """bool [..., V] -> int32 words"""
+    V = bits.shape[-1]
+    W = (V + 31) // 32
+    full = np.zeros(bits.shape[:-1] + (W * 32,), bool)
+    full[..., :V] = bits
+    return np.packbits(full, axis=-1, bitorder="little").view("<i4")
+
+
+class Rows:
+    def __init__(self, B, V, dtype="f32", seed=0, share=None, k=None, p=None, q=None, temps=None, std=2.0, noise=True):
+        r = np.random.default_rng(seed)
+        self.B, self.V = B, V
+        self.logits = torch.from_numpy((std * r.standard_normal((B, V))).astype(np.float32)).to(DT[dtype])
+        self.bits = None if share is None else r.random((B, V)) < share
+        self.noise = np.maximum(r.exponential(size=(B, V)), 1e-20).astype(np.float32) if noise else None
+        self.k = None if k is None else np.resize(np.array(k, np.int32), B)
+        self.p = None if p is None else np.resize(np.array(p, np.float32), B)
+        self.q = None if q is None else np.resize(np.array(q, np.float32), B)
+        self.temps = None if temps is None else np.resize(np.array(temps, np.float32), B)
+
+    def run(self, G, **kw):
+        def dev(x):
+            return None if x is None else torch.from_numpy(np.ascontiguousarray(x)).cuda()
+        args = dict(mask=None if self.bits is None else dev(pack(self.bits)), temperature=dev(self.temps), top_k=dev(self.k),
+                    top_p=dev(self.p), min_p=dev(self.q), noise=dev(self.noise))
+        logits = kw.pop("logits", None)
+        args.update(kw)
+        return G.sample(self.logits.cuda() if logits is None else logits, **args)
+
+    def reference(self):
+        tokens, logp, tol = np.full(self.B, -1), np.zeros(self.B), np.zeros(self.B)
+        close, kept_of = np.zeros(self.B, bool), [None] * self.B
+        l = self.logits.double().numpy()
+        for b in range(self.B):
+            ids = np.arange(self.V) if self.bits is None else self.bits[b].nonzero()[0]
+            x = l[b, ids]
+            if len(x) == 0 or np.isnan(x).any() or not np.isfinite(x.max()):
+                continue
+            T = 1.0 if self.temps is None else float(self.temps[b])
+            cold = self.noise is None or not T > 0
+            down = np.argsort(-x, kind="stable")
+            ids, x = ids[down], x[down]
+            w = np.exp((x - x[0]) / (1.0 if cold else T))
+            n = len(w)
+            if cold:
+                t, z = 0, w.sum()
+            else:
+                if self.k is not None and self.k[b] > 0:
+                    n = min(n, int(self.k[b]))
+                if self.p is not None and self.p[b] < 1:
+                    upto = np.cumsum(w[:n])
+                    all_, want = upto[-1], float(max(self.p[b], 0)) * upto[-1]
+                    before = upto - w[:n]
+                    m = max(1, int((before < want).sum()))
+                    close[b] |= bool((np.abs(before[1:] - want) < 1e-5 * np.minimum(w[1:n], 1e-1 * all_)).any())
+                    n = m
+                if self.q is not None and self.q[b] > 0:
+                    low = min(float(self.q[b]), 1.0)
+                    n = max(1, int((w[:n] >= low).sum()))
+                    close[b] |= bool((np.abs(w[1:] - low) < 1e-5 * low).any())
+                z = w[:n].sum()
+                score = w[:n] / self.noise[b, ids[:n]].astype(np.float64)
+                t = int(score.argmax())
+                close[b] |= bool((np.delete(score, t) > score[t] * (1 - 1e-5)).any())
+            tokens[b], kept_of[b] = ids[t], ids[:n]
+            d = (x[t] - x[0]) / (1.0 if cold else T)
+            logp[b] = d - math.log(z)
+            tol[b] = 2.0 ** -22 * (abs(d) + abs(math.log(z)) + 1) + 2.0 ** -14.6
+        return tokens, logp, tol, close, kept_of
+
+    def check(self, G, may_be_close=0, **kw):
+        tokens, logp, tol, close, _ = self.reference()
+        assert close.sum() <= may_be_close, "inputs that rounding decides"
+        got = [x.cpu().numpy() for x in self.run(G, **kw)]
+        far = ~close
+        assert np.array_equal(got[0][far], tokens[far]), (got[0][far], tokens[far])
+        assert (np.abs(got[1] - logp)[far] <= tol[far]).all(), np.abs(got[1] - logp)[far].max()
+
+
+FILTERS = {"none": {}, "k": {"k": [1, 2, 7, 50, 0, -3, 1000]}, "p": {"p": [0.9, 0.5, 0.99, 0.0, 1.0, 2.0, 0.05]},
+           "q": {"q": [0.1, 0.0, 0.5, 1.0, -1.0, 3.0, 0.01]},
+           "all": {"k": [40, 0, 5, 1000, 3], "p": [0.9, 0.95, 1.0, 0.6], "q": [0.0, 0.02, 0.3]}}
+
+
+@pytest.mark.parametrize("V", [1, 2, 7, 8, 9, 31, 33, 64, 511, 1000, 8191, 8192, 8193, 32000, 50257, 151936])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("filters", list(FILTERS))
+def test_filters(G, V, dtype, filters):
+    Rows(9, V, dtype, seed=V, temps=[0.7, 1.0, 1.3, 0.0], **FILTERS[filters]).check(G, may_be_close=1)
+
+
+@pytest.mark.parametrize("share", [0.0, 2e-4, 0.03, 0.6, 1.0])
+@pytest.mark.parametrize("V", [5, 1000, 50257])
+@pytest.mark.parametrize("filters", ["none", "all"])
+def test_masks(G, share, V, filters):
+    for dtype in DT:
+        Rows(8, V, dtype, seed=V + 1, share=share, temps=[0.9, 1.2], **FILTERS[filters]).check(G, may_be_close=1)
+
+
+@pytest.mark.parametrize("std", [0.0, 1e-3, 0.3, 30.0])
+@pytest.mark.parametrize("V", [600, 40001, 151936])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_flat_and_sharp_rows(G, std, V, dtype):
+    """rows of all equal logits, of few values with many ties at every cut, nuclei of nearly all tokens, and of one"""
+    Rows(6, V, dtype, seed=V + 2, std=std, k=[0, 300, 20000], p=[0.9, 0.97], q=[0.0, 0.5]).check(G, may_be_close=2)
+
+
+def test_ties_at_the_cut_go_to_the_lowest_indexes(G):
+    """many equal logits, of which the cut keeps some: the token is always among the first of them"""
+    B, V = 32, 9000
+    x = Rows(B, V, seed=5, k=[10, 100, 1500])
+    x.logits = torch.full((B, V), -3.0)
+    x.logits[:, 4000:8000] = 1.0
+    x.logits[:, 100:103] = 2.0
+    tokens, _, _, _, kept = x.reference()
+    for b in range(B):
+        k = int(x.k[b])
+        assert set(kept[b]) == set(range(100, 103)) | set(range(4000, 4000 + k - 3))
+    x.check(G)
+
+
+def test_zero_is_zero(G):
+    """-0 and 0 are equal: the lower index comes first"""
+    x = Rows(40, 64, seed=6, k=[1, 3])
+    x.logits = torch.zeros((40, 64))
+    x.logits[:, ::2] *= -1.0
+    x.check(G)
+    x.temps = np.zeros(40, np.float32)
+    assert bool((x.run(G)[0] == 0).all())
+
+
+def test_rows_without_a_distribution(G):
+    V = 300
+    x = Rows(8, V, "f32", seed=7, k=[20], p=[0.9])
+    bits = np.random.default_rng(1).random((8, V)) < 0.5
+    bits[0] = False
+    bits[1:6, 17] = True
+    x.logits[1, 17] = math.nan
+    x.logits[2, 17] = math.inf
+    x.logits[3][torch.from_numpy(bits[3])] = -math.inf
+    x.logits[4, ~torch.from_numpy(bits[4])] = math.nan   # masked: has no part
+    x.logits[5, ~torch.from_numpy(bits[5])] = math.inf
+    x.logits[6, 5] = -math.inf
+    x.bits = bits
+    x.noise[4][~bits[4]] = math.nan
+    got = [y.cpu() for y in x.run(G)]
+    assert got[0][:4].tolist() == [-1] * 4 and got[1][:4].tolist() == [0.0] * 4
+    assert bool((got[0][4:] >= 0).all())
+    x.check(G)
+    x.noise[7] = math.inf  # no weight over noise is above 0
+    assert int(x.run(G)[0][7]) == -1
+
+
+def test_noise_of_what_is_left_out_is_not_used(G):
+    x = Rows(6, 5000, "bf16", seed=8, k=[30], p=[0.9], q=[0.01])
+    want = x.run(G)
+    _, _, _, _, kept = x.reference()
+    for b in range(6):
+        out = np.setdiff1d(np.arange(5000), kept[b])
+        x.noise[b, out] = math.nan
+    got = x.run(G)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_greedy(G):
+    for dtype in DT:
+        x = Rows(7, 3001, dtype, seed=9, share=0.4, noise=False, k=[3], p=[0.5])
+        x.check(G)
+        y = Rows(7, 3001, dtype, seed=9, share=0.4, temps=[0.0, -1.0, math.nan], k=[3], p=[0.5])
+        y.logits = x.logits
+        y.bits = x.bits
+        got, want = y.run(G), x.run(G)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_strides_outputs_and_alignment(G):
+    for dtype in DT:
+        for at in range(4):
+            x = Rows(5, 1023, dtype, seed=10 + at, share=0.5, k=[50], p=[0.95])
+            want = x.run(G)
+            wide = torch.full((5, 1100), math.nan, dtype=DT[dtype], device="cuda")
+            wide[:, at:at + 1023] = x.logits.cuda()
+            mask = torch.full((5, 40), -1, dtype=torch.int32, device="cuda")
+            mask[:, 3:35] = torch.from_numpy(pack(x.bits)).cuda()
+            noise = torch.full((5, 1030), math.nan, device="cuda")
+            noise[:, at:at + 1023] = torch.from_numpy(x.noise).cuda()
+            tokens, logprobs = torch.zeros(5, dtype=torch.int32, device="cuda"), torch.zeros(5, device="cuda")
+            got = x.run(G, logits=wide[:, at:at + 1023], mask=mask[:, 3:35], noise=noise[:, at:at + 1023], tokens=tokens,
+                        logprobs=logprobs)
+            assert got[0] is tokens and got[1] is logprobs
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_bits_past_the_vocabulary_are_not_trusted(G):
+    x = Rows(4, 70, seed=11, share=0.5, k=[5])
+    want = x.run(G)
+    mask = torch.from_numpy(pack(x.bits)).cuda()
+    mask[:, 2] |= -64
+    got = x.run(G, mask=mask)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("seed", range(3))
+def test_tokens_follow_the_distribution(G, seed):
+    """what is drawn in many rows of one distribution against its probabilities, six standard deviations wide"""
+    V, B = 50, 60000
+    r = np.random.default_rng(seed)
+    one = torch.from_numpy(r.standard_normal((1, V)).astype(np.float32))
+    x = Rows(1, V, seed=seed, k=[[20], [0], [12]][seed], p=[[0.9], [0.8], [1.0]][seed], temps=[1.3])
+    x.logits = one
+    kept = x.reference()[4][0]
+    w = np.exp(one.double().numpy()[0, kept] / 1.3)
+    prob = np.zeros(V)
+    prob[kept] = w / w.sum()
+    logits = one.cuda().expand(B, V).contiguous()
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    noise = torch.empty((B, V), device="cuda").exponential_(generator=gen).clamp_min_(1e-20)
+    full = {n: torch.full((B,), float(v[0]), device="cuda") for n, v in (("top_p", x.p), ("temperature", x.temps))}
+    tokens, _ = G.sample(logits, noise=noise, top_k=torch.full((B,), int(x.k[0]), dtype=torch.int32, device="cuda"), **full)
+    share = torch.bincount(tokens.long(), minlength=V).double().cpu().numpy() / B
+    assert (np.abs(share - prob) <= 6 * np.sqrt(prob * (1 - prob) / B) + 1e-12).all()
+
+
+def test_many_rows_other_stream_and_graph(G):
+    x = Rows(700, 2000, "bf16", seed=12, share=0.7, k=[50, 0], p=[0.9, 1.0, 0.5])
+    want = x.run(G)
+    x.check(G, may_be_close=3)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = x.run(G, stream=side)
+    side.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    logits, noise = x.logits.cuda(), torch.from_numpy(x.noise).cuda()
+    mask, k = torch.from_numpy(pack(x.bits)).cuda(), torch.from_numpy(x.k).cuda()
+    graph = torch.cuda.CUDAGraph()
+    tokens, logprobs = torch.empty_like(want[0]), torch.empty_like(want[1])
+    with torch.cuda.graph(graph):
+        G.sample(logits, mask=mask, top_k=k, noise=noise, tokens=tokens, logprobs=logprobs)
+    for i in range(4):
+        noise.exponential_().clamp_min_(1e-20)
+        logits.copy_((2 * torch.randn(logits.shape, device="cuda")).bfloat16())
+        graph.replay()
+        torch.cuda.synchronize()
+        again = G.sample(logits, mask=mask, top_k=k, noise=noise)
+        assert torch.equal(again[0], tokens) and torch.equal(again[1], logprobs)
