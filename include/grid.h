@@ -891,8 +891,9 @@ size_t grid_kv_fork_workspace_bytes(int32_t n_rows, int32_t n_pages);
  * logit, its log p at temperature 1 among all allowed tokens, no filters.
  * A row with no distribution (nothing allowed, or an allowed logit that is NaN or
  * +inf) gives the token -1 and 0; so does one where noise that is not finite
- * leaves no kept token a p / noise above 0 (noise is above 0 and finite; it is
- * read at kept tokens only).  top_p or min_p that is NaN keeps all.
+ * leaves no kept token a p / noise above 0 (noise is above 0 and finite; it has
+ * a part at kept tokens only).  top_p or min_p that is NaN keeps all.  Where
+ * top_k or top_p are in force a p below 2^-60 of the largest counts as 0.
  * Statistics are held in 32 bits or more. */
 typedef struct {
   const void* logits;          /* device [B], rows of V */
@@ -910,8 +911,12 @@ typedef struct {
   int64_t noise_stride;
   int32_t* tokens;             /* device [B] */
   float* logprobs;             /* device [B] */
+  void* workspace;             /* device scratch, 16-byte aligned, grid_sample_workspace_bytes; nothing is expected in it */
+  size_t workspace_bytes;
 } grid_sample_args;
 int grid_sample(const grid_sample_args* args, void* stream);
+/* 0 on bad sizes. */
+size_t grid_sample_workspace_bytes(int32_t B, int32_t V);
 
 #ifdef __cplusplus
 }

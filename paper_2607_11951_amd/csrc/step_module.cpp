@@ -588,9 +588,9 @@ PyObject* kv_fork(PyObject*, PyObject* const* x, Py_ssize_t n) {
   });
 }
 
-// logits, mask, temperature, top_k, top_p, min_p, noise, tokens, logprobs
+// logits, mask, temperature, top_k, top_p, min_p, noise, tokens, logprobs, workspace
 PyObject* sample(PyObject*, PyObject* const* x, Py_ssize_t n) {
-  return guarded(n, 9, [&]() -> PyObject* {
+  return guarded(n, 10, [&]() -> PyObject* {
     const at::Tensor& logits = tensor(x[0], "logits");
     need(logits.dim() == 2 && logits.stride(1) == 1, "logits: [rows, V] with dense rows");
     grid_sample_args a = {};
@@ -623,11 +623,17 @@ PyObject* sample(PyObject*, PyObject* const* x, Py_ssize_t n) {
     const at::Tensor *t = maybe(x[7], "tokens"), *l = maybe(x[8], "logprobs");
     dense(t, at::kInt, {B}, dev, "tokens");
     dense(l, at::kFloat, {B}, dev, "logprobs");
+    const at::Tensor* given_work = maybe(x[9], "workspace");
     no_gradient({&logits, temperature, top_p, min_p, noise, l});
     void* stream = stream_of(dev);
     const c10::DeviceGuard guard(dev);
     const auto ints = logits.options().dtype(at::kInt);
     const at::Tensor tokens = t ? *t : at::empty({B}, ints), logprobs = l ? *l : at::empty({B}, ints.dtype(at::kFloat));
+    const at::Tensor work = given_work ? *given_work
+                                       : at::empty({(int64_t)grid_sample_workspace_bytes(a.B, a.V)}, ints.dtype(at::kByte));
+    need(work.device() == dev && work.is_contiguous(), "workspace: a contiguous tensor on the logits' device");
+    a.workspace = ptr(work);
+    a.workspace_bytes = work.nbytes();
     a.mask = ptr<uint32_t>(mask);
     a.temperature = ptr<float>(temperature);
     a.top_k = ptr<int32_t>(top_k);
@@ -638,7 +644,7 @@ PyObject* sample(PyObject*, PyObject* const* x, Py_ssize_t n) {
     a.logprobs = ptr<float>(logprobs);
     const int rc = grid_sample(&a, stream);
     if (rc != GRID_OK) return PyLong_FromLong(rc);
-    written({t, l});
+    written({t, l, given_work});
     PyObject *p = given(x[7], tokens), *q = given(x[8], logprobs), *both = PyTuple_Pack(2, p, q);
     Py_DECREF(p);
     Py_DECREF(q);

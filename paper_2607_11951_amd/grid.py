@@ -50,7 +50,8 @@ EXPORTS = ["grid_compile", "grid_free", "grid_last_error", "grid_info", "grid_ad
            "grid_complete", "grid_forced_span", "grid_forced_span_workspace_bytes", "grid_kv_append", "grid_attend",
            "grid_attend_workspace_bytes", "grid_verify", "grid_verify_workspace_bytes", "grid_tree_masks",
            "grid_kv_append_tree", "grid_attend_tree", "grid_attend_tree_workspace_bytes", "grid_commit_tree",
-           "grid_kv_copy", "grid_kv_fork", "grid_kv_fork_workspace_bytes", "grid_sample"]
+           "grid_kv_copy", "grid_kv_fork", "grid_kv_fork_workspace_bytes", "grid_sample",
+           "grid_sample_workspace_bytes"]
 CI_LOOKUP, CI_INSERT, CI_FAMILY, CI_GENN = 1, 2, 4, 8
 PHASE_PROLOGUE, PHASE_WALK, PHASE_RESIDUE, PHASE_FINALIZE, PHASE_ALL = 1, 2, 4, 8, 15
 
@@ -144,6 +145,8 @@ def lib():
         L.grid_kv_fork_workspace_bytes.argtypes = [i32, i32]
         L.grid_kv_fork_workspace_bytes.restype = sz
         L.grid_sample.argtypes = [vp, vp]
+        L.grid_sample_workspace_bytes.argtypes = [i32, i32]
+        L.grid_sample_workspace_bytes.restype = sz
         _lib = L
     return _lib
 

@@ -72,7 +72,7 @@ def verify(logits, draft, *, draft_len=None, mask=None, draft_probs=None, unifor
 
 
 def sample(logits, *, mask=None, temperature=None, top_k=None, top_p=None, min_p=None, noise=None, tokens=None,
-           logprobs=None, stream=None):
+           logprobs=None, workspace=None, stream=None):
     """grid_sample: one token of every row of logits [B, V] under the mask rows (int32 [B, words], as Grid.mask writes them;
     None: all tokens allowed), at the rows' temperature (float32 [B]), of the top_k (int32 [B]) largest, of these the ones
     that hold top_p (float32 [B]) of the mass, of these the ones with at least min_p (float32 [B]) of the largest
@@ -81,8 +81,8 @@ def sample(logits, *, mask=None, temperature=None, top_k=None, top_p=None, min_p
     if stream is not None:
         with torch.cuda.stream(stream):
             return sample(logits, mask=mask, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, noise=noise,
-                          tokens=tokens, logprobs=logprobs)
-    return _done(_step.sample(logits, mask, temperature, top_k, top_p, min_p, noise, tokens, logprobs))
+                          tokens=tokens, logprobs=logprobs, workspace=workspace)
+    return _done(_step.sample(logits, mask, temperature, top_k, top_p, min_p, noise, tokens, logprobs, workspace))
 
 
 def tree_masks(parent, cu_q, max_q, *, masks=None, depth=None, stream=None):

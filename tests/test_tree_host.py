@@ -39,7 +39,7 @@ class _Fork(ctypes.Structure):
 class _Sample(ctypes.Structure):
     _fields_ = [("logits", _vp), ("dtype", _i32), ("B", _i32), ("V", _i32), ("logits_stride", _i64), ("mask", _vp),
                 ("mask_stride", _i64), ("temperature", _vp), ("top_k", _vp), ("top_p", _vp), ("min_p", _vp), ("noise", _vp),
-                ("noise_stride", _i64), ("tokens", _vp), ("logprobs", _vp)]
+                ("noise_stride", _i64), ("tokens", _vp), ("logprobs", _vp), ("workspace", _vp), ("workspace_bytes", _sz)]
 
 
 GOOD = {
@@ -48,7 +48,7 @@ GOOD = {
     "commit": lambda: _Commit(AT, AT, AT, None, 7, 2, 1 << 20, 1 << 20, AT, 7, AT, AT),
     "copy": lambda: _Copy(AT, AT, None, 3, 2, 1 << 20, 1 << 20),
     "fork": lambda: _Fork(AT, 5, AT, 3, 4, 5, 100, 16, AT, AT, AT, AT, 2 * AT, 5, 2 * AT, 2 * AT, AT, AT, AT, 1 << 20),
-    "sample": lambda: _Sample(AT, 1, 2, 1000, 1000, AT, 32, None, AT, AT, AT, AT, 1000, AT, AT),
+    "sample": lambda: _Sample(AT, 1, 2, 1000, 1000, AT, 32, None, AT, AT, AT, AT, 1000, AT, AT, AT, 1 << 30),
 }
 
 
@@ -104,7 +104,8 @@ def test_bad_fork(S, name, bad):  # noqa: F811
 
 @pytest.mark.parametrize("name,bad", [("logits", None), ("dtype", 3), ("dtype", -1), ("B", 0), ("B", (1 << 20) + 1), ("V", 0),
                                       ("V", (1 << 30) - 2047), ("logits_stride", -1), ("mask_stride", -1),
-                                      ("noise_stride", -8), ("tokens", None), ("logprobs", None)])
+                                      ("noise_stride", -8), ("tokens", None), ("logprobs", None), ("workspace", None),
+                                      ("workspace", AT + 8), ("workspace_bytes", 4096)])
 def test_bad_sample(S, name, bad):  # noqa: F811
     refused(S, S.lib().grid_sample(by(made("sample", **{name: bad})), None), "grid_sample")
 
@@ -160,6 +161,9 @@ def test_capacities(S):  # noqa: F811
     size = L.grid_kv_fork_workspace_bytes
     assert size(0, 1) == 0 and size(65536, 1) == 0 and size(1, 0) == 0 and size(1, (1 << 26) + 1) == 0
     assert 0 < size(1, 1) <= 1024 and size(65535, 1 << 26) <= (1 << 26) // 8 + 65535 * 32 + (1 << 17)
+    size = L.grid_sample_workspace_bytes
+    assert size(0, 9) == 0 and size(1, 0) == 0 and size((1 << 20) + 1, 9) == 0 and size(1, 1 << 30) == 0
+    assert 0 < size(1, 1) < 1 << 14 and (1 << 27) < size(1 << 20, 151936) <= 1 << 28 and size(1 << 20, 9) < 1 << 28
     assert L.grid_attend_tree_workspace_bytes(by(cache(S)), by(chunks(S)), None) == 0
 
 
