@@ -62,7 +62,7 @@ struct AttendArgs {
   float* lse;
   float2* part_ml;  // [slots][rows of a tile]: maximum (in base 2 units of the scaled score), sum
   float* part_o;    // [slots][rows of a tile][D], not divided by the sum
-  int2* runs;       // [sequences][key heads]: first and last workgroup of the unit (few rows)
+  int2* runs;       // [sequences][key heads][tiles]: first and last workgroup of the unit (shares)
   Divisor group;
   int32_t hq, max_q, max_kv, window;
   // many rows: workgroups; tiles a sequence and key head, ranges of len keys (whole stages); units side by side (kPacked)
@@ -160,7 +160,8 @@ struct Nothing {
 // RW x KW waves: RW * 32 rows, stages of KW * KT keys of which a wave takes KT.
 //  - RW == 1: a wave loads its own keys and waits for nobody.  One stage is held; the next keys are fetched when the
 //    scores have been computed, the next values when the sums have, so loads are in flight all the time.
-//  - RW > 1: the waves share the stages; two are held, the next one is fetched while one is worked on.
+//  - RW > 1: the waves share the stages; two are held, the next one is fetched while one is worked on.  RW > 4: such a workgroup
+//    has a compute unit for itself, and four are held, for one stage on its way is less than the memory's latency asks for.
 // UNI: pages hold whole runs of 16 rows, so the address of a load is a scalar and an offset of the lane.
 template <typename T, int D_, int RW_, int KW_, int KT_, int WGS_, bool UNI_, bool TREE_>
 struct Tile {
@@ -174,7 +175,8 @@ struct Tile {
   static constexpr int RUN = WR < 16 ? WR : 16, RUNS = WR / RUN;  // rows that share a page lookup
   static constexpr int KB = KT / 32, DB = D / 32, QS = D / 16;
   static constexpr uint32_t kHalf = SK * D * 2;  // bytes of a stage's keys
-  static constexpr uint32_t kStages = (PRIV ? 1 : 2) * 2 * kHalf;
+  static constexpr int NB = PRIV ? 1 : RW > 4 ? 4 : 2;  // stages held
+  static constexpr uint32_t kStages = NB * 2 * kHalf;
   static constexpr uint32_t kMerge = KW == 1 ? 0 : KW * TM * (2 + D / 2 + 4) * 4;  // what waves of other keys meet in
   static constexpr uint32_t kLds = kStages > kMerge ? kStages : kMerge;
   typedef typename Vec<T>::eight Eight;
@@ -445,10 +447,50 @@ __device__ __forceinline__ void Tile<T, D_, RW_, KW_, KT_, WGS_, UNI_, TREE_>::r
     const auto torn = [&](int s0) {
       return s0 + SK - 1 > tile_min || s0 + SK > s_hi || (a.window && s0 <= tile_max - a.window);
     };
-    wait_loads<0>();
+    if constexpr (NB > 2)
+#pragma unroll
+      for (int i = 1; i < NB - 1; ++i)
+        if (s_lo + i * SK < s_hi) {
+          fetch(kg, P.ks, base + i * 2 * kHalf);
+          fetch(vg, P.vs, base + i * 2 * kHalf + kHalf);
+          if (s_lo + (i + 1) * SK < s_hi) find(s_lo + (i + 1) * SK);
+        }
+    // stages on their way after the next one: so many, unless they are the last ones
+    const auto arrived = [&](int next) {
+      if (NB > 2 && next + (NB - 2) * SK < s_hi)
+        wait_loads<(NB - 2) * 2 * LOADS>();
+      else
+        wait_loads<0>();
+    };
+    arrived(s_lo);
     if (torn(s_lo)) clean(base + kHalf, s_lo);
     __syncthreads();
     uint32_t buf = 0;
+    if constexpr (NB > 2) {
+      for (int s0 = s_lo; s0 < s_hi; s0 += SK) {
+        if (s0 + (NB - 1) * SK < s_hi) {
+          const uint32_t to = (buf + (NB - 1) * 2 * kHalf) % kStages;
+          fetch(kg, P.ks, base + to);
+          fetch(vg, P.vs, base + to + kHalf);
+          if (s0 + NB * SK < s_hi) find(s0 + NB * SK);
+        }
+        const int k0 = s0 + kw * KT;
+        if (alive && k0 < s_hi && k0 <= pos_max && (!a.window || k0 + KT > pos_min - a.window + 1)) {
+          const uint8_t *ks = lds + buf + kw * KT * D * 2, *vs = ks + kHalf;
+          scores(ks);
+          if (masked(k0)) mask(k0);
+          softmax();
+          sums(vs);
+        }
+        buf = (buf + 2 * kHalf) % kStages;
+        wait_reads();
+        if (s0 + SK < s_hi) {
+          arrived(s0 + SK);
+          if (torn(s0 + SK)) clean(base + buf + kHalf, s0 + SK);
+        }
+        __syncthreads();
+      }
+    } else
     for (int s0 = s_lo; s0 < s_hi; s0 += SK) {
       if (s0 + SK < s_hi) {
         fetch(kg, P.ks, base + (buf ^ 2 * kHalf));
@@ -691,8 +733,8 @@ __device__ inline uint64_t scaled(uint64_t i, uint64_t by, uint64_t over, uint64
   return i * by / over;
 }
 
-// Few rows: every sequence's rows are one tile, and the work is the stages of all sequences and key heads in a row,
-// cut into equal shares: workgroup i takes stages i * total / n .. (i + 1) * total / n - 1, whatever units they belong
+// Few rows, and trees: the work is the stages of all units (a sequence's key head and tile of rows; few rows are one tile) in
+// a row, cut into equal shares: workgroup i takes stages i * total / n .. (i + 1) * total / n - 1, whatever units they belong
 // to.  So all finish together, however ragged the lengths.  Of a unit that workgroups share, the sums of the one that
 // begins it go to its slot 2 i + 1, those of the others to 2 i; runs tells the joining kernel which they are.
 template <typename T, typename X>
@@ -707,6 +749,19 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void shares_kernel(Paged 
   const auto stages = [&](const Chunk& c) {
     return is_bad(a, c) || c.n == 0 ? 0u : (uint32_t)((c.kv - first_key(a, c) + X::SK - 1) / X::SK);
   };
+  constexpr bool kTiles = X::TREE && X::RW >= 4;  // every row of a tree sees its last stage, so a unit's tiles are alike
+  const auto tiles = [&](const Chunk& c) { return kTiles ? (uint32_t)(c.n * (int)a.group.d + X::TM - 1) / X::TM : 1u; };
+  // What a tree's stage counts in the shares, and a unit besides: of eight waves more where they all have rows than where half
+  // of them have none, and to begin a unit costs as much as 3.5 stages.  (Of 32 trees of up to 64 nodes after up to 8128
+  // tokens, 32 heads on 8: 2.1 and 1.6 us a stage and 7.4 a unit.  Where all stages count alike and units nothing 220 us.)
+  constexpr uint32_t kFull = kTiles ? 4 : 1, kHalf = kTiles && X::RW > 4 ? 3 : kFull, kBegin = kTiles ? 14 : 0;
+  const auto last_tile = [&](const Chunk& c) {
+    return c.n * (int)a.group.d - ((int)tiles(c) - 1) * X::TM <= X::TM / 2 ? kHalf : kFull;
+  };
+  const auto counts = [&](const Chunk& c) {  // of a head
+    const uint64_t s = stages(c);
+    return s ? s * (kFull * (tiles(c) - 1) + last_tile(c)) + kBegin * tiles(c) : 0;
+  };
   const bool few = P.B <= 64;  // sequences: a lane each, in every wave; otherwise a run of them each thread
   const int per = few ? 1 : (P.B + X::NT - 1) / X::NT, b0 = min((few ? lane : tid) * per, P.B), b1 = min(b0 + per, P.B);
   Chunk own = {0, 0, 0, false};
@@ -718,7 +773,7 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void shares_kernel(Paged 
       broken = b;
       break;
     }
-    mine += stages(own);
+    mine += counts(own);
   }
   if (few) {
     const uint64_t all = __ballot(broken < P.B);
@@ -753,7 +808,7 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void shares_kernel(Paged 
       const Chunk c = chunk_of(P, b);
       if (is_bad(a, c)) fill_nan<T, X::D>(P, a, c, b, X::NT);
     }
-  uint64_t n = min((uint64_t)gridDim.x, total);  // no share is empty
+  uint64_t n = min((uint64_t)gridDim.x, kFull > 1 ? max(total / kFull, (uint64_t)1) : total);  // no share is empty
   if (me >= n) return;
   uint64_t x = uniform(scaled(total, me, n, total));
   uint64_t end = uniform(scaled(total, me + 1, n, total));
@@ -774,7 +829,7 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void shares_kernel(Paged 
       uint64_t before = upto - mine;
       int i = b0;
       for (; i < b1 - 1; ++i) {
-        const uint32_t s = stages(chunk_of(P, i));
+        const uint64_t s = counts(chunk_of(P, i));
         if (x < (before + s) * heads) break;
         before += s;
       }
@@ -787,21 +842,39 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void shares_kernel(Paged 
     ch = chunk_of(P, b);
   }
   for (;;) {
-    const uint64_t s = stages(ch);
-    if (x >= first + s * heads) {  // the next sequence (b < P.B: x < end <= total)
-      first += s * heads;
+    const uint64_t s = stages(ch), head = kTiles ? counts(ch) : s;
+    if (x >= first + head * heads) {  // the next sequence (b < P.B: x < end <= total)
+      first += head * heads;
       ch = chunk_of(P, ++b);
       continue;
     }
-    const int g = __builtin_amdgcn_readfirstlane((int)((uint32_t)(x - first) / (uint32_t)s));
-    const uint64_t unit = first + (uint64_t)g * s, stop = min(end, unit + s);
-    const bool whole = x == unit && stop == unit + s;
-    if (x == unit && tid == 0)
-      a.runs[(int64_t)b * P.hkv + g] =
-          make_int2((int)me, whole ? (int)me : (int)(((unit + s) * n - 1) / total));
+    const int g = __builtin_amdgcn_readfirstlane((int)((uint32_t)(x - first) / (uint32_t)head));
+    uint64_t unit = first + (uint64_t)g * head;
+    int tile = 0;
+    uint32_t each = 1;  // what a stage counts
+    if constexpr (kTiles) {
+      tile = __builtin_amdgcn_readfirstlane(min((int)((uint32_t)(x - unit) / (kFull * (uint32_t)s + kBegin)), (int)tiles(ch) - 1));
+      each = tile < (int)tiles(ch) - 1 ? kFull : last_tile(ch);
+      unit += (uint64_t)tile * (kFull * s + kBegin);
+    }
+    // a stage is the share's that its first count falls into
+    const uint64_t stop = min(end, unit + kBegin + s * each);
+    const auto begun = [&](uint64_t at) {  // stages before this count
+      return (uint32_t)(max(at, unit + kBegin) - unit - kBegin + each - 1) / each;
+    };
+    const uint32_t from = kTiles ? begun(x) : (uint32_t)(x - unit), to = kTiles ? begun(stop) : (uint32_t)(stop - unit);
+    const bool whole = from == 0 && to == s;
+    if (from == 0 && to > 0 && tid == 0)
+      a.runs[kTiles ? ((int64_t)b * P.hkv + g) * a.tiles + tile : (int64_t)b * P.hkv + g] =
+          make_int2((int)me, whole ? (int)me : (int)(((unit + kBegin + (s - 1) * each + 1) * n - 1) / total));
+    if (kTiles && from == to) {  // (what a unit or its last stage counts besides)
+      x = stop;
+      if (x >= end) return;
+      continue;
+    }
     const int start = first_key(a, ch);
-    const int s_lo = __builtin_amdgcn_readfirstlane(start + (int)(x - unit) * X::SK);
-    const int s_hi = __builtin_amdgcn_readfirstlane(min(ch.kv, start + (int)(stop - unit) * X::SK));
+    const int s_lo = __builtin_amdgcn_readfirstlane(start + (int)from * X::SK);
+    const int s_hi = __builtin_amdgcn_readfirstlane(min(ch.kv, start + (int)to * X::SK));
     // what the loop goes on with waits in LDS: the stages need the scalar registers
     if (tid == 0) {
       kept[0] = stop;
@@ -809,13 +882,13 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void shares_kernel(Paged 
       kept[2] = first;
       kept[3] = total;
     }
-    X::run(P, a, lds, fix, ch, b, g, 0, s_lo, s_hi, whole, (int64_t)me * 2 + (x == unit), Nothing());
+    X::run(P, a, lds, fix, ch, b, g, tile, s_lo, s_hi, whole, (int64_t)me * 2 + (from == 0), Nothing());
     x = uniform(kept[0]);
     end = uniform(kept[1]);
     if (x >= end) return;
     first = uniform(kept[2]);
     total = uniform(kept[3]);
-    n = min((uint64_t)gridDim.x, total);
+    n = min((uint64_t)gridDim.x, kFull > 1 ? max(total / kFull, (uint64_t)1) : total);
     __syncthreads();
     no_fix(fix);
     __syncthreads();
@@ -838,7 +911,7 @@ __global__ __launch_bounds__(256) void join_kernel(Paged P, AttendArgs a) {
   int64_t slots = 0;
   if (live) {
     if constexpr (SHARES) {
-      const int2 run = a.runs[(int64_t)b * P.hkv + g];
+      const int2 run = a.runs[TREE && TM >= 128 ? ((int64_t)b * P.hkv + g) * a.tiles + r / TM : (int64_t)b * P.hkv + g];
       from = run.x;
       to = run.y;
       live = from != to;
@@ -955,7 +1028,7 @@ struct Shape {
   int64_t parts;  // of a row, on average over the units (a long sequence among short ones has more)
   size_t slots;   // of parts
 };
-Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_attend_args* g) {
+Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_attend_args* g, bool tree = false) {
   Shape s;
   const int group = g->n_heads / c->n_kv_heads;
   const int64_t rows = (int64_t)std::min(g->max_q, std::max(1, x->n_tokens)) * group;
@@ -968,20 +1041,21 @@ Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_atten
                        : small >= kComputeUnits / 2 ? 1024
                                                     : 640;
   const bool narrow = small <= 2 * kComputeUnits && span <= few_keys;
-  s.shares = rows <= 64 && !narrow;
+  s.shares = (rows <= 64 || tree) && !narrow;
   s.packed = false;
-  s.tm = rows <= 32 || narrow ? 32
-         : rows <= 64                                                                                  ? 64
-                                                                                                       : 128;
+  s.tm = rows <= 32 || narrow                        ? 32
+         : rows <= 64                                ? 64
+         : tree && rows > 128 && c->head_dim < 256   ? 256
+                                                     : 128;
   s.tiles = (rows + s.tm - 1) / s.tm;
   s.splits = 1;
   s.len = INT32_MAX;
-  s.at_once = (c->head_dim == 256 ? 1 : 2) * kComputeUnits;
+  s.at_once = (c->head_dim == 256 || s.tm == 256 ? 1 : 2) * kComputeUnits;
   if (s.shares) {
     const int64_t stages = (span + kStage - 1) / kStage;
-    s.blocks = std::min<int64_t>(heads * stages, 2 * kComputeUnits);
+    s.blocks = std::min<int64_t>(heads * s.tiles * (stages + (s.tm >= 128 ? 4 : 0)), s.tm >= 128 ? s.at_once : 2 * kComputeUnits);
     s.join = stages > 1;
-    s.parts = s.blocks / heads;
+    s.parts = s.blocks / (heads * s.tiles);
     s.slots = (size_t)s.blocks * 2;
     return s;
   }
@@ -1005,11 +1079,12 @@ Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_atten
   return s;
 }
 
-size_t runs_bytes(const grid_paged_cache* c, const grid_chunks* x) {
-  return ((size_t)x->n_seqs * (size_t)c->n_kv_heads * sizeof(int2) + 15) / 16 * 16;
+size_t runs_bytes(const grid_paged_cache* c, const grid_chunks* x, const Shape& s) {
+  const size_t tiles = s.shares ? (size_t)s.tiles : 1;
+  return ((size_t)x->n_seqs * (size_t)c->n_kv_heads * tiles * sizeof(int2) + 15) / 16 * 16;
 }
 size_t workspace_of(const grid_paged_cache* c, const grid_chunks* x, const Shape& s) {
-  return runs_bytes(c, x) + s.slots * (size_t)s.tm * (size_t)(c->head_dim + 2) * 4;
+  return runs_bytes(c, x, s) + s.slots * (size_t)s.tm * (size_t)(c->head_dim + 2) * 4;
 }
 
 template <typename T, bool TREE, int D, int RW, int KW, int KT, int WGS, bool SHARES>
@@ -1038,9 +1113,11 @@ void launch(const Paged& P, const AttendArgs& a, const Shape& s, hipStream_t str
 // keys for one of 32 took 4 chunks of 2048 tokens after 4096, 8 heads on 1, from 495 us to 400.
 template <typename T, bool TREE>
 void choose(const Paged& P, const AttendArgs& a, const Shape& s, hipStream_t stream) {
-  const auto with = [&](auto few, auto some, auto many, auto narrow) {
-    if (s.tm == 128)
-      many();
+  const auto with = [&](auto few, auto some, auto many, auto narrow, auto most) {
+    if (s.tm == 256)
+      most();
+    else if (s.tm == 128)
+      many(std::integral_constant<bool, TREE>());
     else if (!s.shares)
       narrow();
     else if (s.tm == 32)
@@ -1050,28 +1127,33 @@ void choose(const Paged& P, const AttendArgs& a, const Shape& s, hipStream_t str
   };
   if (P.D == 64)
     with([&] { launch<T, TREE, 64, 1, 4, 32, 2, true>(P, a, s, stream); }, [&] { launch<T, TREE, 64, 2, 2, 32, 2, true>(P, a, s, stream); },
-         [&] { launch<T, TREE, 64, 4, 1, 128, 2, false>(P, a, s, stream); },
-         [&] { launch<T, TREE, 64, 1, 4, 32, 2, false>(P, a, s, stream); });
+         [&](auto shares) { launch<T, TREE, 64, 4, 1, 128, 2, decltype(shares)::value>(P, a, s, stream); },
+         [&] { launch<T, TREE, 64, 1, 4, 32, 2, false>(P, a, s, stream); }, [&] { if constexpr (TREE) launch<T, TREE, 64, 8, 1, 128, 1, true>(P, a, s, stream); });
   else if (P.D == 128)
     with([&] { launch<T, TREE, 128, 1, 4, 32, 2, true>(P, a, s, stream); },
          [&] { launch<T, TREE, 128, 2, 2, 32, 2, true>(P, a, s, stream); },
-         [&] { launch<T, TREE, 128, 4, 1, 64, 2, false>(P, a, s, stream); },
-         [&] { launch<T, TREE, 128, 1, 4, 32, 2, false>(P, a, s, stream); });
+         [&](auto shares) { launch<T, TREE, 128, 4, 1, 64, 2, decltype(shares)::value>(P, a, s, stream); },
+         [&] { launch<T, TREE, 128, 1, 4, 32, 2, false>(P, a, s, stream); }, [&] { if constexpr (TREE) launch<T, TREE, 128, 8, 1, 64, 1, true>(P, a, s, stream); });
   else
     with([&] { launch<T, TREE, 256, 1, 4, 32, 1, true>(P, a, s, stream); },
          [&] { launch<T, TREE, 256, 2, 2, 32, 1, true>(P, a, s, stream); },
-         [&] { launch<T, TREE, 256, 4, 1, 64, 1, false>(P, a, s, stream); },
-         [&] { launch<T, TREE, 256, 1, 4, 32, 1, false>(P, a, s, stream); });
+         [&](auto shares) { launch<T, TREE, 256, 4, 1, 64, 1, decltype(shares)::value>(P, a, s, stream); },
+         [&] { launch<T, TREE, 256, 1, 4, 32, 1, false>(P, a, s, stream); }, [] {});
 }
 
 // The call, whose arguments are checked but for the trees.
 template <bool TREE>
 int attend(const char* call, const grid_paged_cache* cache, const grid_chunks* chunks, const grid_attend_args* args,
            const grid_tree* tree, void* stream) {
-  const Shape s = shape_of(cache, chunks, args);
+  const Shape s = shape_of(cache, chunks, args, TREE);
   if (!args->workspace || (uintptr_t)args->workspace % 16 != 0 ||
       args->workspace_bytes < workspace_of(cache, chunks, s))
     return fail(GRID_E_ARG, std::string(call) + ": workspace too small or not aligned");
+  if (TREE && s.shares && s.tm >= 128) {  // (what the shares count of a sequence, in 32 bits)
+    const int64_t units = (int64_t)cache->n_kv_heads * s.tiles, stages = (span_of(cache, chunks, args) + kStage - 1) / kStage;
+    if (units >= (int64_t)1 << 32 || 4 * stages + 14 >= ((int64_t)1 << 32) / units)
+      return fail(GRID_E_CAPACITY, std::string(call) + ": 2^36 keys of a sequence in all key heads and tiles of rows or more");
+  }
   if (s.blocks > kMostBlocks || (s.join && (int64_t)chunks->n_tokens * args->n_heads > kMostBlocks))
     return fail(GRID_E_CAPACITY, std::string(call) + ": too many rows for one launch");
   AttendArgs a;
@@ -1083,7 +1165,7 @@ int attend(const char* call, const grid_paged_cache* cache, const grid_chunks* c
   }
   a.lse = args->lse;
   a.runs = (int2*)args->workspace;
-  a.part_o = (float*)((uint8_t*)args->workspace + runs_bytes(cache, chunks));
+  a.part_o = (float*)((uint8_t*)args->workspace + runs_bytes(cache, chunks, s));
   a.part_ml = (float2*)(a.part_o + s.slots * (size_t)s.tm * (size_t)cache->head_dim);
   a.group = Divisor((uint32_t)(args->n_heads / cache->n_kv_heads));
   a.hq = args->n_heads;

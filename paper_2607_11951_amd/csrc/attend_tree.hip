@@ -7,7 +7,7 @@ using namespace grid;
 extern "C" size_t grid_attend_tree_workspace_bytes(const grid_paged_cache* cache, const grid_chunks* chunks,
                                                    const grid_attend_args* args) {
   if (check("grid_attend_tree", cache, chunks, args, false) != GRID_OK) return 0;
-  return workspace_of(cache, chunks, shape_of(cache, chunks, args));
+  return workspace_of(cache, chunks, shape_of(cache, chunks, args, true));
 }
 
 extern "C" int grid_attend_tree(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_attend_args* args,
