@@ -1,6 +1,8 @@
 // pages.hip -- grid_kv_copy and grid_kv_fork: the pages of a cache, copied, forked, freed and given out (gfx950).
 //
-// Copies take 16 bytes a lane, 8 in flight, in the order of the page's rows (or heads, where these lie further apart).
+// Copies take 16 bytes a lane, 8 in flight, in the order of the page's rows (or heads, where these lie further apart).  They are
+// bound by bytes: 500 pages of 16 rows, 8 heads of 128, in 32 layers take 412 us, 5.1 TB/s, which is what a plain copy
+// reaches; with accesses that are kept in the caches, 592.
 //
 // A fork is four launches.  The first writes the kept part of the new rows' tables and the reference counts as they were;
 // the second counts: pages that a row's parent keeps for itself, which are nearly all, are neither taken out nor put in.  The
@@ -28,6 +30,7 @@ struct CopyArgs {
   bool rows_inside;
 };
 
+typedef uint32_t Piece __attribute__((ext_vector_type(4)));
 constexpr int kAhead = 8;
 
 __global__ __launch_bounds__(kThreads) void copy_kernel(CopyArgs a) {
@@ -42,7 +45,7 @@ __global__ __launch_bounds__(kThreads) void copy_kernel(CopyArgs a) {
     const uint16_t* from = base + src * a.page_stride[kv];
     uint16_t* to = base + dst * a.page_stride[kv];
     const uint32_t all = (uint32_t)a.page_size * (uint32_t)a.hkv * a.pieces.d;
-    uint4 x[kAhead];
+    Piece x[kAhead];
     int64_t at[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
@@ -50,11 +53,11 @@ __global__ __launch_bounds__(kThreads) void copy_kernel(CopyArgs a) {
       const uint32_t vec = a.pieces.quot(e), piece = e - vec * a.pieces.d, out = a.inner.quot(vec), in = vec - out * a.inner.d;
       const uint32_t r = a.rows_inside ? in : out, h = a.rows_inside ? out : in;
       at[j] = e < all && r < (uint32_t)rows ? r * a.row_stride[kv] + h * a.head_stride[kv] + piece * 8 : -1;
-      if (at[j] >= 0) x[j] = *(const uint4*)(from + at[j]);
+      if (at[j] >= 0) x[j] = __builtin_nontemporal_load((const Piece*)(from + at[j]));
     }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j)
-      if (at[j] >= 0) *(uint4*)(to + at[j]) = x[j];
+      if (at[j] >= 0) __builtin_nontemporal_store(x[j], (Piece*)(to + at[j]));
   }
 }
 
