@@ -352,6 +352,24 @@ __device__ __forceinline__ void whole_row(const SampleArgs& a, const Row& r, Sha
   if (threadIdx.x == 0) write_token(a, r, b, best, best ? (float)row[(int)~(uint32_t)best] : 0.f, m, z);
 }
 
+// A thread's part of a race: its tokens come in order, so of equal scores the first is kept.
+struct Race {
+  float z, score, l;  // the weights' sum; the best score and its logit
+  int t;
+  // logit l, log2 of the weight, noise; weights below `low` are left out
+  __device__ void take(float logit, float log_w, float noise, float low, int token) {
+    const float w = __builtin_amdgcn_exp2f(log_w);
+    if (w < low) return;
+    z += w;
+    const float now = w * __builtin_amdgcn_rcpf(noise);
+    const bool more = now > score;
+    score = more ? now : score;
+    l = more ? logit : l;
+    t = more ? token : t;
+  }
+  __device__ uint64_t key() const { return race_key(score, t); }
+};
+
 // ------------------------------------------------------------------------------------------------------ first launch
 // Bins from this one on hold no cut: what lies so far below the largest weight, V of them at most, is together less than the
 // mass that top_p leaves out.
@@ -430,6 +448,7 @@ __global__ __launch_bounds__(kThreads) void pieces_kernel(SampleArgs a) {
     best = block_sum(sh, best + (uint64_t)__builtin_ldexpf(rest, a.shift));
     mine = tid == 0 ? best : 0;
   } else if (alive && !r.filtered()) {
+    Race race = {0.f, 0.f, 0.f, 0};
 #pragma unroll
     for (int s = 0; s < H; ++s) {
       if (s >= a.steps) continue;
@@ -437,14 +456,20 @@ __global__ __launch_bounds__(kThreads) void pieces_kernel(SampleArgs a) {
       if (!r.greedy) load_noise(a, r, e[s], n);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float l = x[s].at(i, e[s].bits), w = __builtin_amdgcn_exp2f((l - m) * r.c);
-        z += w;
-        const float score = r.greedy ? (l == m ? 1.f : 0.f) : e[s].bits >> i & 1 ? w * __builtin_amdgcn_rcpf(n[i]) : 0.f;
-        const uint64_t key = race_key(score, e[s].from + i);
-        l_best = key > mine ? l : l_best;
-        mine = max(mine, key);
+        const float l = x[s].at(i, e[s].bits);
+        if (r.greedy) {
+          race.z += __builtin_amdgcn_exp2f((l - m) * r.c);
+          const bool more = l == m && race.score == 0.f;
+          race.t = more ? e[s].from + i : race.t;
+          race.score = more ? 1.f : race.score;
+        } else if (e[s].bits >> i & 1) {
+          race.take(l, (l - m) * r.c, n[i], 0.f, e[s].from + i);
+        }
       }
     }
+    mine = race.key();
+    l_best = r.greedy ? m : race.l;
+    z = race.z;
     z = block_sum(sh, z);
     best = block_best(sh, mine);
   }
@@ -489,7 +514,7 @@ __device__ inline Bins bins_of(const SampleArgs& a, const Row& r, int64_t b, flo
         const float part = __builtin_amdgcn_exp2f(-(float)(off % kPerOctave) * (1.f / kPerOctave));
         all += (uint64_t)((double)x.best * __builtin_ldexp((double)part, -(off / kPerOctave)));
       }
-      constexpr int kAhead = 7;  // pieces that are asked for together
+      constexpr int kAhead = 10;  // pieces that are asked for together
       for (int p = 0; p < min(64, a.pieces - p0); p += kAhead) {
         uint64_t y[kAhead];
 #pragma unroll
@@ -778,7 +803,7 @@ struct Listed {
 };
 
 template <typename T>
-__global__ __launch_bounds__(kThreads, 8) void draw_kernel(SampleArgs a) {
+__global__ __launch_bounds__(kThreads, 6) void draw_kernel(SampleArgs a) {
   __shared__ Shared sh;
   __shared__ uint64_t digits[kThreads], held[Listed::kHeldList];
   __shared__ Bins found;
@@ -830,16 +855,20 @@ __global__ __launch_bounds__(kThreads, 8) void draw_kernel(SampleArgs a) {
       f = bins_of(a, r, b, top, own, sh, found);
     else
       __syncthreads();
-    // The piece's tokens: kept, on the list, or neither; none of a piece that lies below the cuts.
-    uint64_t mine = 0;
-    float z = 0.f, l_best = 0.f;
-    const int lowest = r.cuts ? max(f.sure - 1, max(f.k < kBins ? f.k : -1, f.p_to)) : kBins;
+    // The piece's tokens: kept, on the list, or neither; none of a piece that lies below the cuts.  Bins are told by the places
+    // of their edges.
+    const int lowest = max(f.sure - 1, max(f.k < kBins ? f.k : -1, f.p_to));
     const float m_piece = a.piece[b * a.pieces + piece].m;
-    const int steps = top - __builtin_floorf(place(m_piece, r.c)) <= (float)lowest ? a.steps : r.cuts ? 0 : a.steps;
+    const int steps = !r.cuts || top - __builtin_floorf(place(m_piece, r.c)) <= (float)lowest ? a.steps : 0;
+    const float sure = top - (float)f.sure + 1.f, end = top - (float)lowest;  // kept from the one on, listed from the other on
+    const float p_end = top - (float)f.p_to, k_begin = top - (float)f.k + 1.f;  // but between the cuts nothing is
+    Race race = {0.f, 0.f, 0.f, 0};
     constexpr int kAhead = 2;  // steps that are asked for together
     for (int s0 = 0; s0 < steps; s0 += kAhead) {
       Eight e[kAhead];
       Raw<T> x[kAhead];
+      uint32_t kept[kAhead], open[kAhead];
+      float n[kAhead][8];
 #pragma unroll
       for (int s = 0; s < kAhead; ++s)
         e[s] = s0 + s < steps ? eight_of(a, r, (piece * a.steps + s0 + s) * kStep + tid * 8) : Eight{0, 0};
@@ -847,43 +876,43 @@ __global__ __launch_bounds__(kThreads, 8) void draw_kernel(SampleArgs a) {
       for (int s = 0; s < kAhead; ++s) load_eight(a, r, e[s], x[s]);
 #pragma unroll
       for (int s = 0; s < kAhead; ++s) {
-        if (!__any(e[s].bits != 0)) continue;
-        uint32_t kept = e[s].bits;
-        if (r.cuts) {
-          uint32_t open = 0;
-          kept = 0;
+        kept[s] = e[s].bits;
+        open[s] = 0;
+        if (!r.cuts) continue;
+        uint32_t first = 0, some = 0;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float down = top - __builtin_floorf(place(x[s].at(i, e[s].bits), r.c));
-            const int at = (int)fminf(down, (float)kBins);
-            const bool undecided = at < kBins && (at == f.k || (at >= f.p_from && at <= f.p_to));
-            kept |= (uint32_t)(!undecided && at < f.sure) << i;
-            open |= (uint32_t)undecided << i;
-          }
-          for (; open; open &= open - 1) {
-            const int i = __builtin_ctz(open);
-            const uint32_t at = atomicAdd(&listed, 1u);
-            float l = 0.f;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) l = k == i ? x[s].at(k) : l;
-            if (at < (uint32_t)a.room) held[at] = (uint64_t)key_of(l) << 32 | (uint32_t)~(e[s].from + i);
-          }
+        for (int i = 0; i < 8; ++i) {
+          const float at = place(x[s].at(i), r.c);
+          first |= (uint32_t)(at >= sure) << i;
+          some |= (uint32_t)(at >= end && (at >= p_end || at < k_begin)) << i;
         }
-        if (__any(kept != 0)) {
-          float n[8];
-          if (kept) load_noise(a, r, e[s], n);
+        kept[s] = first & e[s].bits;
+        open[s] = some & ~first & e[s].bits;
+      }
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float l = x[s].at(i), w = __builtin_amdgcn_exp2f((l - m) * r.c);
-            if (!(kept >> i & 1) || w < r.low) continue;
-            z += w;
-            const uint64_t key = race_key(w * __builtin_amdgcn_rcpf(n[i]), e[s].from + i);
-            l_best = key > mine ? l : l_best;
-            mine = max(mine, key);
-          }
+      for (int s = 0; s < kAhead; ++s)
+        if (kept[s]) load_noise(a, r, e[s], n[s]);
+#pragma unroll
+      for (int s = 0; s < kAhead; ++s)
+        for (uint32_t left = open[s]; left; left &= left - 1) {
+          const int i = __builtin_ctz(left);
+          const uint32_t at = atomicAdd(&listed, 1u);
+          float l = 0.f;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) l = k == i ? x[s].at(k) : l;
+          if (at < (uint32_t)a.room) held[at] = (uint64_t)key_of(l) << 32 | (uint32_t)~(e[s].from + i);
         }
+#pragma unroll
+      for (int s = 0; s < kAhead; ++s) {
+        if (!__any(kept[s] != 0)) continue;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (kept[s] >> i & 1) race.take(x[s].at(i), (x[s].at(i) - m) * r.c, n[s][i], r.low, e[s].from + i);
       }
     }
+    const uint64_t mine = race.key();
+    const float l_best = race.l;
+    float z = race.z;
     z = block_sum(sh, z);
     const uint64_t best = block_best(sh, mine);
     const int64_t at = b * a.pieces + piece;

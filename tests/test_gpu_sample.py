@@ -272,3 +272,39 @@ def test_many_rows_other_stream_and_graph(G):
         torch.cuda.synchronize()
         again = G.sample(logits, mask=mask, top_k=k, noise=noise)
         assert torch.equal(again[0], tokens) and torch.equal(again[1], logprobs)
+
+
+def test_vocabularies_of_many_pieces(G):
+    Rows(2, 1200001, "bf16", seed=13, k=[0, 700], p=[0.9, 0.95], temps=[1.3, 0.4]).check(G)
+    Rows(2, 1100003, "f32", seed=14, share=0.3).check(G)
+
+
+@pytest.mark.parametrize("temp", [1e-7, 1e-5, 1e-3, 0.05, 20.0, 1e6])
+def test_temperatures(G, temp):
+    """weights that fall by thousands of octaves and weights that are all alike"""
+    for dtype in DT:
+        for V in (50, 20000):
+            Rows(4, V, dtype, seed=15, temps=[temp], k=[0, 40], p=[0.9, 0.9, 1.0], q=[0.0, 0.3]).check(G, may_be_close=2)
+
+
+def test_logits_far_from_zero(G):
+    for shift in (-3e4, 3e4, 1e30):
+        for std in (2.0, 1e4):
+            x = Rows(5, 3000, "f32", seed=16, k=[50, 0], p=[0.9])
+            x.logits = x.logits * std + shift  # (all alike at 1e30: where 0.9 cuts among equals is close to a token's border)
+            x.check(G, may_be_close=3)
+
+
+def test_more_rows_than_a_launch_takes(G):
+    """the workspace holds so many rows: the others follow"""
+    x = Rows(3000, 40, "f32", seed=17, share=0.5, k=[5, 0], p=[0.9], q=[0.0, 0.05])
+    x.check(G, may_be_close=5)
+    big = Rows(1800, 40, "bf16", seed=18, k=[5])
+    want = big.run(G)
+    logits = torch.full((1800, 100000), -math.inf, dtype=torch.bfloat16, device="cuda")
+    logits[:, 50000:50040] = big.logits.cuda()
+    noise = torch.ones((1800, 100000), device="cuda")
+    noise[:, 50000:50040] = torch.from_numpy(big.noise).cuda()
+    got = G.sample(logits, top_k=torch.from_numpy(big.k).cuda(), noise=noise)
+    # (five weights or fewer, added in another order: a relative 8 * 2^-24, and roundings of the logarithm and the difference)
+    assert torch.equal(got[0], want[0] + 50000) and bool(((got[1] - want[1]).abs() <= 2.0 ** -20 * (1 + want[1].abs())).all())
