@@ -30,6 +30,7 @@ constexpr int kStep = kThreads * 8;  // tokens that a workgroup takes at a time
 constexpr int kHeld = 4;               // steps of a piece, at most: what registers hold where two workgroups share a compute unit
 constexpr int kBins = 1024, kPerOctave = 16;
 constexpr int kList = 2048;  // tokens of a piece's bins at the cuts, at most
+constexpr int kTops = kHeld * kWaves;
 constexpr int kDigit = 9;    // bits, a thread for each value
 static_assert(1 << kDigit == kThreads && kBins == 2 * kThreads, "");
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -64,6 +65,7 @@ struct SampleArgs {
   uint32_t* done;  // [B]
   uint64_t* list;  // [B][pieces][room]: key << 32 | complement of the token
   uint64_t* hist;  // [B][pieces][kBins]
+  float* tops;     // [B][pieces][kTops]: the largest logit of a wave's part of a step
 };
 
 // Logits in their order, as whole numbers; -0 is 0.
@@ -402,13 +404,16 @@ __global__ __launch_bounds__(kThreads) void pieces_kernel(SampleArgs a) {
   if (r.cuts)
     for (int i = tid; i < kBins; i += kThreads) hist[i] = 0;
   if (piece == 0 && tid == 0) a.done[b] = 0;
-  float m = -INFINITY;
+  float m = -INFINITY, tops[H];
 #pragma unroll
   for (int s = 0; s < H; ++s) {
     if (s >= a.steps) continue;
+    float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 8; i += 2)
-      m = __builtin_elementwise_maximum(m, __builtin_elementwise_maximum(x[s].at(i, e[s].bits), x[s].at(i + 1, e[s].bits)));
+      top = __builtin_elementwise_maximum(top, __builtin_elementwise_maximum(x[s].at(i, e[s].bits), x[s].at(i + 1, e[s].bits)));
+    tops[s] = top;
+    m = __builtin_elementwise_maximum(m, top);
   }
   m = block_maximum(sh, m);
   float z = 0.f, l_best = 0.f;
@@ -473,6 +478,13 @@ __global__ __launch_bounds__(kThreads) void pieces_kernel(SampleArgs a) {
     z = block_sum(sh, z);
     best = block_best(sh, mine);
   }
+  if (r.cuts)
+#pragma unroll
+    for (int s = 0; s < H; ++s) {
+      if (s >= a.steps) continue;
+      const float top = maximum_across(tops[s]);
+      if ((tid & 63) == 0) a.tops[(b * a.pieces + piece) * kTops + s * kWaves + (tid >> 6)] = top;
+    }
   // (no two threads have the same token)
   if (best ? mine == best : tid == 0) a.piece[b * a.pieces + piece] = {m, z, best, l_best, halves};
 }
@@ -813,6 +825,7 @@ __global__ __launch_bounds__(kThreads, 6) void draw_kernel(SampleArgs a) {
   const Row r = row_of<T>(a, b);
   Piece own = {-INFINITY, 0.f, 0, 0.f, 0};
   if (lane < a.pieces) own = a.piece[b * a.pieces + lane];
+  const float top_lane = r.cuts && lane < kTops ? a.tops[(b * a.pieces + piece) * kTops + lane] : 0.f;
   float m = own.m;
   for (int p = 64 + lane; p < a.pieces; p += 64) m = __builtin_elementwise_maximum(m, a.piece[b * a.pieces + p].m);
   m = maximum_across(m);
@@ -855,25 +868,36 @@ __global__ __launch_bounds__(kThreads, 6) void draw_kernel(SampleArgs a) {
       f = bins_of(a, r, b, top, own, sh, found);
     else
       __syncthreads();
-    // The piece's tokens: kept, on the list, or neither; none of a piece that lies below the cuts.  Bins are told by the places
-    // of their edges.
+    // The piece's tokens: kept, on the list, or neither; a wave's steps that lie below the cuts are not
+    // read.  Bins are told by the places of their edges.
     const int lowest = max(f.sure - 1, max(f.k < kBins ? f.k : -1, f.p_to));
-    const float m_piece = a.piece[b * a.pieces + piece].m;
-    const int steps = !r.cuts || top - __builtin_floorf(place(m_piece, r.c)) <= (float)lowest ? a.steps : 0;
     const float sure = top - (float)f.sure + 1.f, end = top - (float)lowest;  // kept from the one on, listed from the other on
     const float p_end = top - (float)f.p_to, k_begin = top - (float)f.k + 1.f;  // but between the cuts nothing is
     Race race = {0.f, 0.f, 0.f, 0};
     constexpr int kAhead = 2;  // steps that are asked for together
-    for (int s0 = 0; s0 < steps; s0 += kAhead) {
+    uint32_t ask = (1u << a.steps) - 1;
+    if (r.cuts)
+      for (int s = 0; s < kHeld; ++s) {
+        const float highest = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(top_lane), s * kWaves + (tid >> 6)));
+        if (!(place(highest, r.c) >= end)) ask &= ~(1u << s);
+      }
+    while (ask) {
+      int step[kAhead];
+#pragma unroll
+      for (int s = 0; s < kAhead; ++s) {
+        step[s] = ask ? __builtin_ctz(ask) : -1;
+        ask &= ask - 1;
+      }
       Eight e[kAhead];
       Raw<T> x[kAhead];
       uint32_t kept[kAhead], open[kAhead];
       float n[kAhead][8];
 #pragma unroll
       for (int s = 0; s < kAhead; ++s)
-        e[s] = s0 + s < steps ? eight_of(a, r, (piece * a.steps + s0 + s) * kStep + tid * 8) : Eight{0, 0};
+        e[s] = step[s] >= 0 ? eight_of(a, r, (piece * a.steps + step[s]) * kStep + tid * 8) : Eight{0, 0};
 #pragma unroll
-      for (int s = 0; s < kAhead; ++s) load_eight(a, r, e[s], x[s]);
+      for (int s = 0; s < kAhead; ++s)
+        if (step[s] >= 0) load_eight(a, r, e[s], x[s]);
 #pragma unroll
       for (int s = 0; s < kAhead; ++s) {
         kept[s] = e[s].bits;
@@ -998,7 +1022,7 @@ Plan plan(int32_t B, int32_t V) {
   p.steps = (int)((all + pieces - 1) / pieces);
   p.pieces = (int)((all + p.steps - 1) / p.steps);
   p.room = std::min(V, kList);
-  p.row_bytes = (size_t)p.pieces * (kBins * 8 + (size_t)p.room * 8 + sizeof(Left) + sizeof(Piece)) + 8;
+  p.row_bytes = (size_t)p.pieces * (kBins * 8 + (size_t)p.room * 8 + sizeof(Left) + sizeof(Piece) + kTops * 4) + 8;
   p.rows = (int)std::max<size_t>(1, std::min<size_t>((size_t)B, ((size_t)1 << 28) / p.row_bytes));
   return p;
 }
@@ -1042,7 +1066,8 @@ extern "C" int grid_sample(const grid_sample_args* args, void* stream) {
   a.list = a.hist + all * kBins;
   a.left = (Left*)(a.list + all * (size_t)p.room);
   a.piece = (Piece*)(a.left + all);
-  a.done = (uint32_t*)(a.piece + all);
+  a.tops = (float*)(a.piece + all);
+  a.done = (uint32_t*)(a.tops + all * kTops);
   const hipStream_t s = (hipStream_t)stream;
   for (int32_t b = 0; b < g.B; b += p.rows) {
     const int32_t rows = std::min(p.rows, g.B - b);
