@@ -320,3 +320,45 @@ def test_forked_rows_read_what_they_wrote(G):
             for p in host[b][:int(held[b])]:
                 count[p] += 1
         assert refs.tolist() == count.tolist()
+
+
+@pytest.mark.parametrize("R,P", [(32, 16384), (33, 16384), (32, 16385), (300, 9000)])
+def test_fork_in_place_in_either_launch(G, R, P):
+    """one workgroup or four launches: reference counts in place, rows inside larger tables, replayed graphs"""
+    page, cols = 8, 14
+    table, held, lens, refs = world(R, page, cols, P, R, 80)
+    r = random.Random(R)
+    parent = [r.choice([b, b, r.randrange(R), -1]) for b in range(R)]
+    keep = [0 if p < 0 else r.choice([lens[p], lens[p] // 2]) for p in parent]
+    room = [k + r.choice([0, 1, 20]) for k in keep]
+    want = plain_fork(table, held, parent, keep, room, refs, page)
+    wide = torch.full((R, 20), -9, dtype=torch.int32, device="cuda")
+    wide[:, 3:3 + cols] = ints(table)
+    out = torch.full((R, 30), 77, dtype=torch.int32, device="cuda")
+    counts, start = ints(refs), ints(refs)
+    args = (wide[:, 3:3 + cols], ints(held), ints(parent), ints(keep), ints(room), counts, page)
+    kw = dict(table_out=out[:, 5:5 + cols], refs_out=counts)
+    got = G.kv_fork(*args, **kw)
+    for x, y in zip(got, want):
+        assert x.tolist() == y
+    assert bool((out[:, :5] == 77).all()) and bool((out[:, 5 + cols:] == 77).all())
+    kw.update(held_out=got[1], copies=got[3], status=got[4], workspace=torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        G.kv_fork(*args, **kw)
+    for _ in range(4):
+        counts.copy_(start)
+        for x in (out, *got[1:2], *got[3:]):
+            x.fill_(55)
+        kw["workspace"].fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip((out[:, 5:5 + cols], got[1], counts, got[3], got[4]), want):
+            assert x.tolist() == y
+    side = torch.cuda.Stream()
+    counts.copy_(start)
+    torch.cuda.synchronize()
+    got = G.kv_fork(*args[:6], page, stream=side)
+    side.synchronize()
+    for x, y in zip(got, want):
+        assert x.tolist() == y

@@ -547,3 +547,47 @@ def test_a_step_with_trees(G):
         for s in range(kv_ - n + len(p)):
             page, row = (int(x[0]) for x in bt.rows(b, np.array([s])))
             assert torch.equal(one[0][page, row], two[0][page, row]) and torch.equal(one[1][page, row], two[1][page, row])
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 128), (6, 3, 64), (4, 1, 256)])
+@pytest.mark.parametrize("B", [63, 64, 65, 150])
+def test_many_sequences(G, heads, B):
+    """shares of ragged trees over long and short caches, empty chunks among them"""
+    r = random.Random(B)
+    lens = []
+    for i in range(B):
+        n = r.choice([0, 1, 2, 9, 40, 64, 64 // (heads[0] // heads[1]) + 1])
+        lens.append((n, n + r.choice([0, 1, 63, 64, 65, 300, r.randint(0, 2500)])))
+    lens[B // 2] = (64, 2600)
+    bt = Trees(lens, heads, 16, "bf16", seed=B)
+    got = bt.attend(G)
+    agree(got, bt)
+    again = bt.attend(G, max_kv=1 << 20)
+    agree(again, bt)
+    # a chunk out of order: it and all after it are bad
+    bt.cu[B // 2 + 1] = 0
+    got = bt.attend(G)
+    first = int(bt.cu_host[B // 2])
+    assert bool(torch.isnan(got[0][first:].float()).all()) and bool(torch.isfinite(got[0][:first].float()).all())
+
+
+def test_offsets_past_32_bits(G):
+    """a cache of more than 2^32 entries: the sequence's pages lie at its end"""
+    page, H, D = 64, 8, 128
+    P = (1 << 32) // (page * H * D) + 40
+    bt = Trees([(40, 1500)], (16, H, D), page, "bf16", seed=15)
+    n = bt.k.shape[0]
+    big_k, big_v = (torch.empty((P, page, H, D), dtype=bt.dt, device="cuda") for _ in range(2))
+    big_k[-n:], big_v[-n:] = bt.k, bt.v
+    want = bt.attend(G)
+    table = bt.table + (P - n)
+    got = G.attend_tree(bt.q, big_k, big_v, table, bt.kv_len, bt.cu, bt.tree, bt.max_q, bt.max_kv)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    tokens, said = list(range(bt.T)), [-1] * bt.T
+    for i in range(1, bt.T):
+        said[bt.parent[i]] = tokens[i]
+    args = (bt.kv_len, bt.cu, ints(tokens), ints(bt.parent), ints(said), bt.max_q)
+    one = G.commit_tree(big_k, big_v, table, *args)
+    two = G.commit_tree(bt.k, bt.v, bt.table, *args)
+    assert all(torch.equal(x, y) for x, y in zip(one, two))
+    assert torch.equal(big_k[-n:], bt.k) and torch.equal(big_v[-n:], bt.v)
