@@ -2,7 +2,8 @@
 //
 // Copies take 16 bytes a lane, 8 in flight, in the order of the page's rows (or heads, where these lie further apart).  They are
 // bound by bytes: 500 pages of 16 rows, 8 heads of 128, in 32 layers take 412 us, 5.1 TB/s, which is what a plain copy
-// reaches; with accesses that are kept in the caches, 592.
+// reaches; with accesses that are kept in the caches, 592.  A workgroup moves 32 KiB, of small pages several pairs: 1000 pages of
+// one row, 4 heads of 128, in 48 layers take 39 us, a workgroup a pair 124.
 //
 // A fork of few rows in a small pool is one workgroup's, with the reference counts in LDS.  Otherwise it is four launches.  The first writes the kept part of the new rows' tables and the reference counts as they were;
 // the second counts: pages that a row's parent keeps for itself, which are nearly all, are neither taken out nor put in.  The
@@ -26,39 +27,50 @@ struct CopyArgs {
   const int32_t *src, *dst, *rows;
   int64_t page_stride[2], row_stride[2], head_stride[2], layer_stride[2];  // keys', values'
   Divisor parts, inner, pieces;  // workgroups a page and layer; heads (or rows) of a row (or head); pieces of a vector
-  int64_t units;                 // in all: pairs, layers, keys and values, parts
-  int32_t page_size, hkv, n_pages, layers, n;
+  Divisor whole;                 // pieces of a page and layer
+  int64_t units;                 // in all: groups of pairs, layers, keys and values, parts
+  int32_t page_size, hkv, n_pages, layers, n, group;  // group: pairs that a workgroup takes together (small pages)
   bool rows_inside;
 };
 
 typedef uint32_t Piece __attribute__((ext_vector_type(4)));
 constexpr int kAhead = 8;
 
+// GROUPS: pages of so few pieces that a workgroup takes several pairs.
+template <bool GROUPS>
 __global__ __launch_bounds__(kThreads) void copy_kernel(CopyArgs a) {
   const int tid = (int)threadIdx.x;
   for (int64_t u = blockIdx.x; u < a.units; u += gridDim.x) {
-    const int64_t whole = u / a.parts.d;
-    const int part = (int)(u - whole * a.parts.d), kv = (int)(whole & 1);
-    const int i = (int)((whole >> 1) / a.layers), layer = (int)((whole >> 1) - (int64_t)i * a.layers);
-    const int src = a.src[i], dst = a.dst[i], rows = a.rows ? min(max(a.rows[i], 0), a.page_size) : a.page_size;
-    if ((uint32_t)src >= (uint32_t)a.n_pages || (uint32_t)dst >= (uint32_t)a.n_pages || src == dst) continue;
+    const int64_t upper = u / a.parts.d;
+    const int part = (int)(u - upper * a.parts.d), kv = (int)(upper & 1);
+    const int first = (int)((upper >> 1) / a.layers), layer = (int)((upper >> 1) - (int64_t)first * a.layers);
     uint16_t* base = (kv ? a.v : a.k) + layer * a.layer_stride[kv];
-    const uint16_t* from = base + src * a.page_stride[kv];
-    uint16_t* to = base + dst * a.page_stride[kv];
-    const uint32_t all = (uint32_t)a.page_size * (uint32_t)a.hkv * a.pieces.d;
     Piece x[kAhead];
-    int64_t at[kAhead];
+    Piece* to[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      const uint32_t e = (uint32_t)part * (kThreads * kAhead) + (uint32_t)(j * kThreads + tid);
-      const uint32_t vec = a.pieces.quot(e), piece = e - vec * a.pieces.d, out = a.inner.quot(vec), in = vec - out * a.inner.d;
-      const uint32_t r = a.rows_inside ? in : out, h = a.rows_inside ? out : in;
-      at[j] = e < all && r < (uint32_t)rows ? r * a.row_stride[kv] + h * a.head_stride[kv] + piece * 8 : -1;
-      if (at[j] >= 0) x[j] = __builtin_nontemporal_load((const Piece*)(from + at[j]));
+      uint32_t e = (uint32_t)part * (kThreads * kAhead) + (uint32_t)(j * kThreads + tid);
+      int i = first;
+      bool in = true;
+      if constexpr (GROUPS) {
+        const uint32_t sub = a.whole.quot(e);
+        e -= sub * a.whole.d;
+        i = first * a.group + (int)sub;
+        in = (int)sub < a.group && i < a.n;
+        i = min(i, a.n - 1);
+      }
+      const int src = a.src[i], dst = a.dst[i], rows = a.rows ? min(max(a.rows[i], 0), a.page_size) : a.page_size;
+      in = in && (uint32_t)src < (uint32_t)a.n_pages && (uint32_t)dst < (uint32_t)a.n_pages && src != dst && e < a.whole.d;
+      const uint32_t vec = a.pieces.quot(e), piece = e - vec * a.pieces.d, out = a.inner.quot(vec), at = vec - out * a.inner.d;
+      const uint32_t r = a.rows_inside ? at : out, h = a.rows_inside ? out : at;
+      in = in && r < (uint32_t)rows;
+      const int64_t offset = r * a.row_stride[kv] + h * a.head_stride[kv] + piece * 8;
+      to[j] = in ? (Piece*)(base + dst * a.page_stride[kv] + offset) : nullptr;
+      if (in) x[j] = __builtin_nontemporal_load((const Piece*)(base + src * a.page_stride[kv] + offset));
     }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j)
-      if (at[j] >= 0) __builtin_nontemporal_store(x[j], (Piece*)(to + at[j]));
+      if (to[j]) __builtin_nontemporal_store(x[j], to[j]);
   }
 }
 
@@ -433,13 +445,19 @@ extern "C" int grid_kv_copy(const grid_paged_cache* cache, const grid_copy_args*
   const int64_t all = (int64_t)cache->page_size * cache->n_kv_heads * (cache->head_dim / 8);
   if (all >= (int64_t)1 << 30) return fail(GRID_E_CAPACITY, "grid_kv_copy: a page has 2^30 pieces of 16 bytes or more");
   a.parts = Divisor((uint32_t)((all + kThreads * kAhead - 1) / (kThreads * kAhead)));
-  a.units = (int64_t)g.n * g.n_layers * 2 * a.parts.d;
+  a.whole = Divisor((uint32_t)all);
+  a.group = (int32_t)std::max<int64_t>(1, kThreads * kAhead / all);
+  a.units = (int64_t)((g.n + a.group - 1) / a.group) * g.n_layers * 2 * a.parts.d;
   a.page_size = cache->page_size;
   a.hkv = cache->n_kv_heads;
   a.n_pages = cache->n_pages;
   a.layers = g.n_layers;
   a.n = g.n;
-  hipLaunchKernelGGL(copy_kernel, dim3((unsigned)std::min<int64_t>(a.units, 1 << 20)), dim3(kThreads), 0, (hipStream_t)stream, a);
+  const dim3 blocks((unsigned)std::min<int64_t>(a.units, 1 << 20));
+  if (a.group > 1)
+    hipLaunchKernelGGL(copy_kernel<true>, blocks, dim3(kThreads), 0, (hipStream_t)stream, a);
+  else
+    hipLaunchKernelGGL(copy_kernel<false>, blocks, dim3(kThreads), 0, (hipStream_t)stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(GRID_E_HIP, std::string("grid_kv_copy launch: ") + hipGetErrorString(e));
   return GRID_OK;
