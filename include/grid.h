@@ -55,7 +55,8 @@ extern "C" {
                                        viable configuration never has an empty mask */
 #define GRID_ROW_BAD_CONFIG 2       /* state, slot or stack out of range */
 #define GRID_ROW_OVERFLOW 4         /* a per-lane parser overlay capacity was exceeded;
-                                       the row's mask is not exact */
+                                       the row's mask is not exact.  grid_kv_fork: no
+                                       pages left for the row */
 #define GRID_ROW_NOT_VIABLE 8       /* grid_accept: the token is not allowed at the
                                        configuration (the prefix would leave Prefix(L)) */
 #define GRID_ROW_FINISHED 16        /* grid_accept: the end-of-sequence token was accepted */
@@ -546,7 +547,7 @@ size_t grid_forced_span_workspace_bytes(const grid_compiled* g, int32_t B);
 /* -------------------------------------------------------------------- apply */
 #define GRID_DTYPE_F32 0
 #define GRID_DTYPE_BF16 1
-#define GRID_DTYPE_F16 2   /* grid_kv_append, grid_attend and grid_verify only */
+#define GRID_DTYPE_F16 2   /* the calls of a model's step only, from grid_kv_append on */
 /* In place: logits[b * row_stride + t] = -inf for every t < V whose mask bit
  * is 0 (fp32 0xFF800000, bf16 0xFF80); other entries keep their bit patterns
  * (section 2: hard -inf masking, a soundness precondition of Proposition 7).

@@ -13,6 +13,13 @@
 //
 // A row whose list is too long (nearly all logits alike), or whose exponents are out of all bounds, is taken by one
 // workgroup, digit by digit over the row itself.
+//
+// Bounds.  256 rows of 50257 in float32 have 51 MB to read, 10 us; the launches take 20 and 38 us, of which the rows alone
+// are 14, a workgroup's vector units being busy half of the time; then noise and what a flat nucleus lists, ordered by
+// digits.  32 rows of 151936 in bf16 take 11 and 18 us, one 6 and 12: some ten dependent reads in two launches, and the
+// pieces' histograms, which every workgroup of a row adds up for itself (a launch that did it once would cost what it
+// saves).  A workgroup remembers each wave's largest logit of a step, so waves whose tokens are all below the cuts do not read
+// them again: of the 256 rows 54 us for 65.
 #include <algorithm>
 #include <string>
 #include <type_traits>
@@ -1009,8 +1016,10 @@ __global__ __launch_bounds__(kThreads, 6) void draw_kernel(SampleArgs a) {
   whole_row<T>(a, r, sh, b, m);
 }
 
-// The launches.  Rows are cut into pieces so that there are about 512 workgroups, what runs at once, none of less than a
-// step and none of more than registers hold.  So many rows share a pair of launches that the workspace stays below 256 MiB.
+// The launches.  Rows are cut into pieces so that there are about 320 workgroups, none of less than two steps unless the row is
+// shorter, and none of more than registers hold (512, 640 and 1024 workgroups, what runs at once and more, were within 2 us:
+// each piece more is a histogram more).  So many rows share a pair of launches that the workspace stays below 256 MiB, or
+// is one row's.
 struct Plan {
   int pieces, steps, room, rows;
   size_t row_bytes;

@@ -6,8 +6,8 @@
 // moves its columns of the rows: a thread has the same 16 bytes of all rows, so those it writes are those it has read before.
 //
 // The masks are bound by a handful of dependent reads, and so is the commit of few sequences.  64 trees of up to 64 nodes, 8
-// heads of 128 in 32 layers, take 17 us: 6 until the branches are known, then their bytes (rows that the caches keep, which
-// nobody reads soon: 21 us).
+// heads of 128 in 32 layers, take 15.7 us: 6 until the branches are known, then their bytes (with rows that the caches keep,
+// which nobody reads soon, 21.3).
 #include <algorithm>
 #include <string>
 
