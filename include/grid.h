@@ -764,8 +764,9 @@ int grid_kv_append_tree(const grid_paged_cache* cache, const grid_chunks* chunks
  * its chunk the places j whose bit is set in masks[t * stride_words + j / 32]:
  * as grid_tree_masks writes them, or any others.  The rest is as there (the
  * calls have workspaces of their own; GRID_E_CAPACITY for 2^36 keys times key
- * heads and tiles of 256 rows too); a row that sees nothing is 0, its lse -inf.  With a window depth is not NULL, and a depth counts as at least 0 and
- * less than the chunk. */
+ * heads and tiles of 256 rows too); a row that sees nothing is 0, its lse -inf.
+ * With a window depth is not NULL, and a depth counts as at least 0 and less
+ * than the chunk. */
 typedef struct {
   const uint32_t* masks;   /* device [n_tokens][stride_words], >= ceil(min(max_q, n_tokens) / 32) words each */
   int64_t stride_words;
