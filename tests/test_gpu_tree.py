@@ -379,6 +379,25 @@ def test_append_leaves_out_depths_without_a_position(G):
                 rounded_once(got[None], want, size)
 
 
+@pytest.mark.parametrize("at", [0, 15, 16, 63, 64, 127, 128, 500, 999])
+def test_append_tells_where_a_depth_has_no_position(G, at):
+    """at a place of every tree that has it, in some a negative depth, in the others one past the table of positions"""
+    lens = [(1, 3), (64, 70), (128, 200), (129, 129), (0, 5), (1000, 1024), (600, 700), (128, 128), (17, 30)] * 8
+    bt = Trees(lens, (1, 1, 64), 16, "bf16", seed=at)
+    k = bt.rand((bt.T, 1, 64))
+    cos, sin = tables(1024, 64)
+    status = torch.full((len(lens),), -1, dtype=torch.int32, device="cuda")
+    for bad in (None, -1, 1024):
+        depth, want = torch.zeros_like(bt.depth), []
+        for b, (n, kv) in enumerate(lens):
+            hit = bad is not None and n > at and b % 3 != 0
+            want.append(2 if hit else 0)
+            if hit:
+                depth[int(bt.cu_host[b]) + at] = bad
+        G.kv_append(k, k, bt.k, bt.v, bt.table, bt.kv_len, bt.cu, cos=cos, sin=sin, depth=depth, status=status)
+        assert status.tolist() == want
+
+
 # ------------------------------------------------------------------------------------------------------------ commit
 def plain_commit(bt, tokens, parent, said, start, max_q):
     paths, nexts = [], []
