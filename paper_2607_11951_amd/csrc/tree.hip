@@ -1,13 +1,15 @@
 // tree.hip -- grid_tree_masks and grid_commit_tree: what a step with a tree of drafts needs before and after the model (gfx950).
 //
-// A node comes after its parent, so a chain of parents is one of falling places: the words of a node's ancestors are written
-// from the highest down as the chain is followed, a thread a node.  The branch that the target's tokens follow is found by a
-// wave, 64 places a step, while the others look up the chunk's pages; every workgroup of a sequence finds it for itself, and
-// moves its columns of the rows: a thread has the same 16 bytes of all rows, so those it writes are those it has read before.
+// A node comes after its parent, so a chain of parents is one of falling places.  A wave takes 64 places and finds the
+// ancestors among these of each, twice as many a step, and the first ancestor before them; a node's words are then those of
+// at most one place in every 64.  For the branch that the target's tokens follow each node tells its parent if it is such a
+// child, the lowest place counts, and the path is followed; every workgroup of a sequence does so for itself, and moves
+// its columns of the rows: a thread has the same 16 bytes of all rows, so those it writes are those it has read before.
 //
-// The masks are bound by a handful of dependent reads, and so is the commit of few sequences.  64 trees of up to 64 nodes, 8
-// heads of 128 in 32 layers, take 15.7 us: 6 until the branches are known, then their bytes (with rows that the caches keep,
-// which nobody reads soon, 21.3).
+// The masks are bound by a handful of dependent reads (32 trees of 64 nodes 4 us, one of 1024, a chain, 21; followed place by
+// place 134), and so is the commit of few sequences (a chain of 64 nodes, all kept, 7 us; with a search of the chunk a node 20).
+// 64 trees of up to 64 nodes, 8 heads of 128 in 32 layers, take 14 us: 5 until the branches are known, then their bytes (with
+// rows that the caches keep, which nobody reads soon, 5 more).
 #include <algorithm>
 #include <string>
 
@@ -19,6 +21,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMost = 1024;  // nodes of a tree
+constexpr int kNone = 0x7FFFFFFF;
 typedef uint32_t Piece __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------------------------------------------------------- masks
@@ -31,30 +34,44 @@ struct MaskArgs {
 };
 
 __global__ __launch_bounds__(kThreads) void masks_kernel(Paged P, MaskArgs a) {
-  __shared__ int32_t up[kMost];
-  const int b = (int)blockIdx.x, tid = (int)threadIdx.x;
+  __shared__ uint64_t bits[kMost];  // a place and its ancestors among its 64
+  __shared__ int32_t out[kMost];    // the first ancestor before these, -1: none
+  const int b = (int)blockIdx.x, tid = (int)threadIdx.x, lane = tid & 63;
   const int32_t first = P.cu_q[b], end = P.cu_q[b + 1];
   const OrderBefore before(P, b, tid);
   if (__syncthreads_or(!before.ok(P, b, tid, kThreads))) return;  // the first that is not in order has these rows
   const bool ordered = in_order(P, first, end), tree = ordered && end - first <= a.max_q;
   const int from = min(max(first, 0), P.T), n = (ordered ? end : P.T) - from;
   if (tree) {
-    for (int i = tid; i < n; i += kThreads) {
-      const int32_t p = a.parent[from + i];
-      up[i] = p >= 0 && p < i ? p : -1;
+    for (int base = tid & ~63; base < n; base += kThreads) {
+      const int i = base + lane;
+      int p = i < n ? a.parent[from + i] : -1;
+      if (p < 0 || p >= i) p = -1;
+      // x: the places from i up to q, the next ancestor's lane (-1: all of them); p: then the first before
+      uint64_t x = 1ull << lane;
+      int q = p >= base ? p - base : -1;
+      while (__any(q >= 0)) {
+        const int next = q >= 0 ? q : lane;
+        const uint64_t y = (uint64_t)__shfl((unsigned long long)x, next);
+        const int out_of = __shfl(p, next), after = __shfl(q, next);
+        if (q >= 0) x |= y, p = out_of, q = after;
+      }
+      if (i < n) bits[i] = x, out[i] = p;
     }
     __syncthreads();
   }
   for (int i = tid; i < n; i += kThreads) {
     uint32_t* words = a.masks + (int64_t)(from + i) * a.stride;
     int at = tree ? i : -1, deep = -1;
-    for (int w = a.words - 1; w >= 0; --w) {
-      uint32_t x = 0;
-      for (; at >= w * 32; at = up[at]) {
-        x |= 1u << (at & 31);
-        ++deep;
+    for (int w = (a.words - 1) / 2; w >= 0; --w) {
+      uint64_t x = 0;
+      if (at >= w * 64) {
+        x = bits[at];
+        at = out[at];
+        deep += __builtin_popcountll(x);
       }
-      words[w] = x;
+      words[2 * w] = (uint32_t)x;
+      if (2 * w + 1 < a.words) words[2 * w + 1] = (uint32_t)(x >> 32);
     }
     a.depth[from + i] = max(deep, 0);
   }
@@ -71,7 +88,7 @@ struct CommitArgs {
 
 // A workgroup a sequence, a layer and a part of the columns (16-byte pieces of a row of keys and values).
 __global__ __launch_bounds__(kThreads) void commit_kernel(Paged P, CommitArgs a) {
-  __shared__ int32_t up[kMost], token[kMost], said[kMost], path[kMost], page[kMost];
+  __shared__ int32_t up[kMost], said[kMost], child[kMost], path[kMost], page[kMost];  // child: that the branch takes, or kNone
   __shared__ int found;
   const int tid = (int)threadIdx.x, lane = tid & 63;
   const int part = (int)(blockIdx.x % (uint32_t)a.parts), b = (int)(blockIdx.x / (uint32_t)a.parts), layer = (int)blockIdx.y;
@@ -82,15 +99,28 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(Paged P, CommitArgs a)
   if (c.ok && a.layers > 0) c = chunk_of(P, first, end, P.kv_len[b]);
   const int from = a.start ? a.start[b] : 0;
   const int n = c.ok && c.n <= a.max_q && from >= 0 && from < c.n ? c.n : 0;
-  for (int i = tid; i < n; i += kThreads) {
+  constexpr int kEach = kMost / kThreads;
+  int32_t token[kEach];
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int i = tid + k * kThreads;
+    token[k] = -1;
+    if (i >= n) continue;
     const int32_t p = a.parent[first + i];
+    token[k] = a.tokens[first + i];
     up[i] = p >= 0 && p < i ? p : -1;
-    token[i] = a.tokens[first + i];
     said[i] = a.sampled[first + i];
+    child[i] = kNone;
     if (a.layers > 0) {
       uint32_t row;
       page[i] = P.page_of(b, (uint32_t)(c.kv - c.n + i), row);
     }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int i = tid + k * kThreads;
+    if (token[k] >= 0 && up[i] >= 0 && said[up[i]] == token[k]) atomicMin(&child[up[i]], i);
   }
   __syncthreads();
   if (tid < 64) {
@@ -102,17 +132,14 @@ __global__ __launch_bounds__(kThreads) void commit_kernel(Paged P, CommitArgs a)
         --j;
         if (lane == 0) path[j] = i;
       }
-      for (at = from;;) {
-        const int want = said[at];
-        int child = -1;
-        for (int i = at + 1; want >= 0 && i < n && child < 0; i += 64) {
-          const uint64_t hit = __ballot(i + lane < n && up[min(i + lane, n - 1)] == at && token[min(i + lane, n - 1)] == want);
-          if (hit) child = i + __builtin_ctzll(hit);
-        }
-        if (child < 0) break;
-        at = child;
-        if (lane == 0) path[length] = at;
-        ++length;
+      at = from;
+      if (n <= 64) {
+        const int mine = lane < n ? child[lane] : kNone;
+        for (int c; (c = __builtin_amdgcn_readlane(mine, at)) != kNone; at = c, ++length)
+          if (lane == 0) path[length] = c;
+      } else {
+        for (int c; (c = child[at]) != kNone; at = c, ++length)
+          if (lane == 0) path[length] = c;
       }
     }
     if (lane == 0) {

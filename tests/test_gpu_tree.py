@@ -464,6 +464,26 @@ def test_commit(G, lens, page, heads):
     assert torch.equal(one_k, both_k[0]) and torch.equal(one_v, both_v[0])
 
 
+@pytest.mark.parametrize("n", [2, 63, 64, 65, 128, 257, 1000])
+@pytest.mark.parametrize("reach", [1, 2, 70])
+def test_branches_to_the_end(G, n, reach):
+    """every child matches, so that the branch is the first children's down to a leaf (of a chain all of it)"""
+    lens = [(n, n + 5), (1, 1), (n, n)]
+    bt = Trees(lens, (2, 1, 64), 16, "bf16", seed=n + reach, reach=reach)
+    tokens, said = [0] * bt.T, [0] * bt.T
+    for start in ([0, 0, 0], [n - 1, 0, n // 2]):
+        paths, nexts = plain_commit(bt, tokens, bt.parent, said, start, bt.max_q)
+        assert reach > 1 or [len(p) for p in paths] == [n, 1, n]
+        path, length, following = G.commit_tree(None, None, None, None, bt.cu, ints(tokens), ints(bt.parent), ints(said),
+                                                bt.max_q, start=ints(start))
+        assert path.tolist() == [p + [-1] * (bt.max_q - len(p)) for p in paths]
+        assert length.tolist() == [len(p) for p in paths] and following.tolist() == nexts
+    # tokens and targets that are no tokens match nothing
+    minus = ints([-1] * bt.T)
+    _, length, following = G.commit_tree(None, None, None, None, bt.cu, minus, ints(bt.parent), minus, bt.max_q)
+    assert length.tolist() == [1, 1, 1] and following.tolist() == [-1, -1, -1]
+
+
 def test_commit_layouts_and_outputs(G):
     """heads before rows, layers inside pages, outputs that are given, a graph"""
     lens = [(20, 50), (7, 300)]
