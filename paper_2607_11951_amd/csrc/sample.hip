@@ -36,7 +36,7 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kStep = kThreads * 8;  // tokens that a workgroup takes at a time
 constexpr int kHeld = 4;               // steps of a piece, at most: what registers hold where two workgroups share a compute unit
 constexpr int kBins = 1024, kPerOctave = 16;
-constexpr int kList = 2048;  // tokens of a piece's bins at the cuts, at most
+constexpr int kList = 4096;  // tokens of a piece's bins at the cuts, at most
 constexpr int kTops = kHeld * kWaves;
 constexpr int kDigit = 9;    // bits, a thread for each value
 static_assert(1 << kDigit == kThreads && kBins == 2 * kThreads, "");
@@ -626,7 +626,7 @@ struct Listed {
   int64_t b;
   float m, top;
   uint32_t n;
-  static constexpr int kHeldList = 2048;
+  static constexpr int kHeldList = kList;
   static constexpr int kShift = 46;  // masses are w * 2^kShift, relative to the upper edge of the highest bin on the list
 
   __device__ int highest() const { return min(f.k, f.p_from); }
@@ -659,10 +659,12 @@ struct Listed {
       for (uint32_t i = threadIdx.x; i < n; i += kThreads) g(held[i]);
       return;
     }
-    for (int p = 0; p < a.pieces; ++p) {
+    // (a wave a piece: 151936 tokens, std 0.6, a nucleus of 0.9 62 us for 89, the pieces one after the other)
+    for (int p = (int)threadIdx.x >> 6; p < a.pieces; p += kWaves) {
       const int64_t at = b * a.pieces + p;
       const uint32_t have = (uint32_t)__hip_atomic_load(&a.left[at].listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      for (uint32_t i = threadIdx.x; i < have; i += kThreads)
+#pragma unroll 4
+      for (uint32_t i = threadIdx.x & 63; i < have; i += 64)
         g(__hip_atomic_load(a.list + at * a.room + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
     }
   }
