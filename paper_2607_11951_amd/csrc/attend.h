@@ -1004,7 +1004,12 @@ int check(const std::string& call, const grid_paged_cache* cache, const grid_chu
 
 // The launch.
 //  - Trees of more than 128 rows: tiles of 256 (heads of 256: 128), one workgroup of eight waves a compute unit, and equal
-//    shares of all tiles' stages (32 ragged trees of up to 64 nodes, 32 heads on 8: 159 us, whole tiles of 128 253).
+//    shares of all tiles' stages (32 ragged trees of up to 64 nodes, 32 heads on 8: 159 us, whole tiles of 128 253).  With
+//    less than 6 stages for a workgroup tiles of 128, of which two share a compute unit (one of 64 nodes after 2048 tokens:
+//    26.2 us and 29.7, after 8192 33.2 and 36.7).  Few keys and tiles of 128 that fill the chip: those, whole, as to begin a
+//    unit costs more than what lengths differ by (ragged, up to 64 nodes, 32 heads on 8: 32 trees, up to 512 keys 28 us and 49,
+//    1024 44 and 58, 4096 134 and 118; 128, 512 81 and 129; 4096 under a window of 1365 59 and 82; 64, 8 heads on 1 of 256,
+//    512 34 and 46, 1024 56 and 57).
 //  - Up to 64 rows a sequence and key head: one tile of 32 or 64, and equal shares of the stages, two workgroups a compute
 //    unit, or fewer where there are fewer stages.
 //  - More rows: tiles of 128; where they are fewer than 3/4 of the workgroups that run at once the keys are split, into
@@ -1024,6 +1029,7 @@ int check(const std::string& call, const grid_paged_cache* cache, const grid_chu
 //    keys, all seen, 15.7 and 20.4, 2048 25.8 and 24.1; 4 chunks of 100, 28 heads on 4, 1024 22.6 and 28.9, 2048 36.5 and
 //    34.4; 2 of 128 with heads of 256, 1024 28.8 and 33.3, 2048 47.6 and 36.3.
 constexpr int kComputeUnits = 256;
+constexpr int kFewStages = 6;
 constexpr int64_t kMostBlocks = (int64_t)1 << 23;  // of a launch: below 2^32 threads
 struct Shape {
   int tm, splits, len;
@@ -1046,12 +1052,16 @@ Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_atten
                        : small >= kComputeUnits / 2 ? 1024
                                                     : 640;
   const bool narrow = small <= 2 * kComputeUnits && span <= few_keys;
-  s.shares = (rows <= 64 || tree) && !narrow;
+  // trees of more rows: the stages of tiles of 256 and of 128, and whether whole tiles of 128 do
+  const int64_t at_once = (c->head_dim == 256 ? 1 : 2) * kComputeUnits, units = heads * ((rows + 127) / 128);
+  const int64_t wide = heads * ((rows + 255) / 256) * ((span + kStage - 1) / kStage);
+  const bool whole = tree && rows > 64 && !narrow && units >= at_once && units <= kMostBlocks && span <= (g->window ? 2048 : 1024);
+  s.shares = (rows <= 64 || tree) && !narrow && !whole;
   s.packed = false;
-  s.tm = rows <= 32 || narrow                        ? 32
-         : rows <= 64                                ? 64
-         : tree && rows > 128 && c->head_dim < 256   ? 256
-                                                     : 128;
+  s.tm = rows <= 32 || narrow                                                                         ? 32
+         : rows <= 64                                                                                 ? 64
+         : tree && !whole && rows > 128 && c->head_dim < 256 && wide >= kFewStages * kComputeUnits     ? 256
+                                                                                                      : 128;
   s.tiles = (rows + s.tm - 1) / s.tm;
   s.splits = 1;
   s.len = INT32_MAX;
@@ -1122,7 +1132,7 @@ void choose(const Paged& P, const AttendArgs& a, const Shape& s, hipStream_t str
     if (s.tm == 256)
       most();
     else if (s.tm == 128)
-      many(std::integral_constant<bool, TREE>());
+      s.shares ? many(std::integral_constant<bool, TREE>()) : many(std::integral_constant<bool, false>());
     else if (!s.shares)
       narrow();
     else if (s.tm == 32)

@@ -610,6 +610,39 @@ def test_many_sequences(G, heads, B):
     assert bool(torch.isnan(got[0][first:].float()).all()) and bool(torch.isfinite(got[0][:first].float()).all())
 
 
+@pytest.mark.parametrize("heads", [(8, 2, 128), (6, 3, 64), (4, 1, 256), (28, 4, 128)])
+@pytest.mark.parametrize("page,window", [(16, 0), (24, 0), (16, 150), (100, 1900)])
+def test_many_trees_of_short_texts(G, heads, page, window):
+    """so many that whole tiles fill the chip; under a window after longer texts too"""
+    r = random.Random(page)
+    lens, most = [], 1024 if window == 0 else 3000
+    for i in range(190):
+        n = r.choice([0, 1, 2, 31, 33, 63, 64])
+        lens.append((n, n + r.choice([0, 1, 63, 64, 65, 300, r.randint(0, most - 64)]) if n else 0))
+    lens[7], lens[100] = (64, most), (64, 64)
+    bt = Trees(lens, heads, page, "bf16", seed=page)
+    got = bt.attend(G, window=window)
+    agree(got, bt, window=window)
+    again = bt.attend(G, window=window)
+    assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1])
+    # what is not seen has no part: free pages
+    used = torch.zeros(bt.k.shape[:2], dtype=torch.bool)
+    for b, (n, kv) in enumerate(lens):
+        if kv:
+            page_of, row = bt.rows(b, np.arange(kv))
+            used[torch.from_numpy(np.asarray(page_of)).long(), torch.from_numpy(np.asarray(row)).long()] = True
+    used = used.cuda()
+    bt.k[~used] = math.nan
+    bt.v[~used] = math.nan
+    again = bt.attend(G, window=window)
+    assert torch.equal(again[0], got[0]) and torch.equal(again[1], got[1])
+    # a chunk out of order: it and all after it are bad
+    bt.cu[101] = 0
+    got = bt.attend(G, window=window)
+    first = int(bt.cu_host[100])
+    assert bool(torch.isnan(got[0][first:].float()).all()) and bool(torch.isfinite(got[0][:first].float()).all())
+
+
 def test_offsets_past_32_bits(G):
     """a cache of more than 2^32 entries: the sequence's pages lie at its end"""
     page, H, D = 64, 8, 128
