@@ -811,7 +811,10 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void shares_kernel(Paged 
       const Chunk c = chunk_of(P, b);
       if (is_bad(a, c)) fill_nan<T, X::D>(P, a, c, b, X::NT);
     }
-  uint64_t n = min((uint64_t)gridDim.x, kFull > 1 ? max(total / kFull, (uint64_t)1) : total);  // no share is empty
+  // No share is empty, and where nothing has a stage (no new tokens, or bad sequences alone) there are none: a unit counts
+  // kBegin and a stage's kHalf at least, so total / kFull is 0 only if total is.
+  static_assert(kBegin + kHalf >= kFull, "");
+  uint64_t n = min((uint64_t)gridDim.x, total / kFull);
   if (me >= n) return;
   uint64_t x = uniform(scaled(total, me, n, total));
   uint64_t end = uniform(scaled(total, me + 1, n, total));
@@ -891,7 +894,7 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void shares_kernel(Paged 
     if (x >= end) return;
     first = uniform(kept[2]);
     total = uniform(kept[3]);
-    n = min((uint64_t)gridDim.x, kFull > 1 ? max(total / kFull, (uint64_t)1) : total);
+    n = min((uint64_t)gridDim.x, total / kFull);
     __syncthreads();
     no_fix(fix);
     __syncthreads();
