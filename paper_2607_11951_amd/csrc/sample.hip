@@ -626,24 +626,27 @@ struct Listed {
   int64_t b;
   float m, top;
   uint32_t n;
+  // Masses are w * 2^shift, relative to the upper edge of the highest bin on the list, so a weight is 1 and a rounding at
+  // most: the sum of n is below 2^63 and a few roundings.
+  int shift;
   static constexpr int kHeldList = kList;
-  static constexpr int kShift = 46;  // masses are w * 2^kShift, relative to the upper edge of the highest bin on the list
+  static __device__ int shift_of(uint32_t n) { return min(46, 31 + __builtin_clz(n | 1u)); }
 
   __device__ int highest() const { return min(f.k, f.p_from); }
   __device__ float edge() const { return (top - (float)highest() + 1.f) * (1.f / kPerOctave); }
   static __device__ float logit(uint64_t x) { return value_of((uint32_t)(x >> 32)); }
   __device__ int bin(uint64_t x) const { return (int)fminf(top - __builtin_floorf(place(logit(x), r.c)), (float)kBins); }
   __device__ uint64_t mass(uint64_t x) const {
-    return (uint64_t)__builtin_ldexpf(__builtin_amdgcn_exp2f(__builtin_fmaf(logit(x), r.c, -edge())), kShift);
+    return (uint64_t)__builtin_ldexpf(__builtin_amdgcn_exp2f(__builtin_fmaf(logit(x), r.c, -edge())), shift);
   }
   // The mass of the listed tokens that top_p keeps, where top_k keeps so much of its bin.
   __device__ uint64_t target(uint64_t k_mass) const {
     // the list's masses relative to the row's
     const double unit = __builtin_ldexp((double)__builtin_amdgcn_exp2f(-(float)(highest() % kPerOctave) * (1.f / kPerOctave)),
-                                        a.shift - highest() / kPerOctave - kShift);
+                                        a.shift - highest() / kPerOctave - shift);
     const double all = f.k < kBins ? (double)f.k_before + (double)k_mass * unit : (double)f.all;
     const double want = __builtin_ceil(((double)r.top_p * all - (double)f.p_before) / unit);
-    return want > 1.0 ? (uint64_t)want : 1;
+    return want > 1.0 ? (uint64_t)fmin(want, 0x1.8p63) : 1;  // (more than all there is: all)
   }
   __device__ float score(uint64_t x) const {
     const float w = __builtin_amdgcn_exp2f((logit(x) - m) * r.c);
@@ -996,7 +999,7 @@ __global__ __launch_bounds__(kThreads, 6) void draw_kernel(SampleArgs a) {
       l = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(l), __builtin_ctzll(owner)));
       z = sum_across(z);
       __syncthreads();
-      const Listed x = {a, r, sh, digits, held, f, b, m, top, (uint32_t)n};
+      const Listed x = {a, r, sh, digits, held, f, b, m, top, (uint32_t)n, Listed::shift_of((uint32_t)n)};
       uint64_t best = 0, mass = 0;
       float l_listed = 0.f;
       if (n <= Listed::kAlone && tid >= 64) return;
@@ -1007,7 +1010,7 @@ __global__ __launch_bounds__(kThreads, 6) void draw_kernel(SampleArgs a) {
       else
         mass = x.by_digits(best, l_listed);
       if (tid > 0) return;
-      z += (float)((double)mass * __builtin_ldexp(1.0, -Listed::kShift)) * __builtin_amdgcn_exp2f(__builtin_fmaf(-m, r.c, x.edge()));
+      z += (float)((double)mass * __builtin_ldexp(1.0, -x.shift)) * __builtin_amdgcn_exp2f(__builtin_fmaf(-m, r.c, x.edge()));
       if (best > first)
         write_token(a, r, b, best, l_listed, m, z);
       else
