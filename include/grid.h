@@ -751,6 +751,12 @@ typedef struct {
   int32_t* depth;          /* device [n_tokens] */
 } grid_tree_args;
 int grid_tree_masks(const grid_tree_args* args, void* stream);
+/* The same under a sliding window of `window` positions (0: none): of t and its
+ * ancestors only the nearest `window` have bits, those of depth > depth[t] -
+ * window.  With these bits and the same window grid_attend_tree sees of a branch
+ * what grid_attend sees of a chunk; a tree that is no deeper than the window has
+ * the same bits without it. */
+int grid_tree_masks_window(const grid_tree_args* args, int32_t window, void* stream);
 
 /* grid_kv_append for trees: keys and queries are rotated by the position first
  * + depth[t] (first: the cached tokens before the chunk), and lie at first +
@@ -761,8 +767,9 @@ int grid_kv_append_tree(const grid_paged_cache* cache, const grid_chunks* chunks
 
 /* grid_attend for trees.  Token t sees the cached tokens before its chunk
  * (with a window w > 0 of these the positions s > first + depth[t] - w), and of
- * its chunk the places j whose bit is set in masks[t * stride_words + j / 32]:
- * as grid_tree_masks writes them, or any others.  The rest is as there (the
+ * its chunk the places j whose bit is set in masks[t * stride_words + j / 32],
+ * whatever the window: as grid_tree_masks or, of trees that may be deeper than the
+ * window, grid_tree_masks_window writes them, or any others.  The rest is as there (the
  * calls have workspaces of their own; GRID_E_CAPACITY for 2^36 keys times key
  * heads and tiles of 256 rows too); a row that sees nothing is 0, its lse -inf.
  * With a window depth is not NULL, and a depth counts as at least 0 and less

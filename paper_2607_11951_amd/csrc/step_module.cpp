@@ -387,9 +387,9 @@ PyObject* verify(PyObject*, PyObject* const* x, Py_ssize_t n) {
   });
 }
 
-// parent, cu_q, max_q, masks, depth
+// parent, cu_q, max_q, masks, depth, window
 PyObject* tree_masks(PyObject*, PyObject* const* x, Py_ssize_t n) {
-  return guarded(n, 5, [&]() -> PyObject* {
+  return guarded(n, 6, [&]() -> PyObject* {
     const at::Tensor &parent = tensor(x[0], "parent"), &cu_q = tensor(x[1], "cu_q");
     const at::Device dev = parent.device();
     need(parent.dim() == 1, "parent: [tokens]");
@@ -401,6 +401,8 @@ PyObject* tree_masks(PyObject*, PyObject* const* x, Py_ssize_t n) {
     a.n_seqs = small(cu_q.size(0) - 1, "cu_q");
     a.max_q = whole(x[2], "max_q");
     need(a.max_q >= 1, "max_q");
+    const int32_t window = whole(x[5], "window");
+    need(window >= 0, "window");
     const int64_t T = parent.size(0), words = ((int64_t)a.max_q + 31) / 32;
     const at::Tensor *m = maybe(x[3], "masks"), *d = maybe(x[4], "depth");
     if (m)
@@ -417,7 +419,7 @@ PyObject* tree_masks(PyObject*, PyObject* const* x, Py_ssize_t n) {
     a.masks = ptr<uint32_t>(masks);
     a.stride_words = T > 1 ? masks.stride(0) : masks.size(1);
     a.depth = ptr<int32_t>(depth);
-    const int rc = grid_tree_masks(&a, stream);
+    const int rc = window ? grid_tree_masks_window(&a, window, stream) : grid_tree_masks(&a, stream);
     if (rc != GRID_OK) return PyLong_FromLong(rc);
     written({m, d});
     PyObject *p = given(x[3], masks), *q = given(x[4], depth), *both = PyTuple_Pack(2, p, q);

@@ -30,7 +30,7 @@ struct MaskArgs {
   uint32_t* masks;
   int32_t* depth;
   int64_t stride;
-  int32_t max_q, words;
+  int32_t max_q, words, window;  // window: bits of a node, the nearest ancestors', at most
 };
 
 __global__ __launch_bounds__(kThreads) void masks_kernel(Paged P, MaskArgs a) {
@@ -69,6 +69,8 @@ __global__ __launch_bounds__(kThreads) void masks_kernel(Paged P, MaskArgs a) {
         x = bits[at];
         at = out[at];
         deep += __builtin_popcountll(x);
+        // the lowest places are the furthest ancestors: what lies past the window goes
+        for (int past = min(deep + 1 - a.window, __builtin_popcountll(x)); past > 0; --past) x &= x - 1;
       }
       words[2 * w] = (uint32_t)x;
       if (2 * w + 1 < a.words) words[2 * w + 1] = (uint32_t)(x >> 32);
@@ -200,10 +202,10 @@ static Paged no_cache(const int32_t* cu_q, int32_t n_seqs, int32_t n_tokens) {
   return p;
 }
 
-extern "C" int grid_tree_masks(const grid_tree_args* args, void* stream) {
-  clear_error();
-  auto bad = [](const char* what) { return fail(GRID_E_ARG, std::string("grid_tree_masks: ") + what); };
+static int tree_masks(const std::string& call, const grid_tree_args* args, int32_t window, void* stream) {
+  auto bad = [&](const char* what) { return fail(GRID_E_ARG, call + ": " + what); };
   if (!args) return bad("null argument");
+  if (window < 0) return bad("window");
   const grid_tree_args& g = *args;
   if (g.n_seqs < 1 || g.n_seqs > 65535) return bad("1 to 65535 sequences");
   if (g.n_tokens < 0 || g.n_tokens > 1 << 24) return bad("n_tokens");
@@ -220,10 +222,21 @@ extern "C" int grid_tree_masks(const grid_tree_args* args, void* stream) {
   a.stride = g.stride_words;
   a.max_q = g.max_q;
   a.words = (g.max_q + 31) / 32;
+  a.window = window ? window : kMost;
   hipLaunchKernelGGL(masks_kernel, dim3((unsigned)g.n_seqs), dim3(kThreads), 0, (hipStream_t)stream, P, a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return fail(GRID_E_HIP, std::string("grid_tree_masks launch: ") + hipGetErrorString(e));
+  if (e != hipSuccess) return fail(GRID_E_HIP, call + " launch: " + hipGetErrorString(e));
   return GRID_OK;
+}
+
+extern "C" int grid_tree_masks(const grid_tree_args* args, void* stream) {
+  clear_error();
+  return tree_masks("grid_tree_masks", args, 0, stream);
+}
+
+extern "C" int grid_tree_masks_window(const grid_tree_args* args, int32_t window, void* stream) {
+  clear_error();
+  return tree_masks("grid_tree_masks_window", args, window, stream);
 }
 
 extern "C" int grid_commit_tree(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_commit_args* args,

@@ -49,6 +49,7 @@ EXPORTS = ["grid_compile", "grid_free", "grid_last_error", "grid_info", "grid_ad
            "grid_accept_inplace", "grid_ci_cache_bytes", "grid_ci_cache_clear", "grid_mask_warm",
            "grid_complete", "grid_forced_span", "grid_forced_span_workspace_bytes", "grid_kv_append", "grid_attend",
            "grid_attend_workspace_bytes", "grid_verify", "grid_verify_workspace_bytes", "grid_tree_masks",
+           "grid_tree_masks_window",
            "grid_kv_append_tree", "grid_attend_tree", "grid_attend_tree_workspace_bytes", "grid_commit_tree",
            "grid_kv_copy", "grid_kv_fork", "grid_kv_fork_workspace_bytes", "grid_sample",
            "grid_sample_workspace_bytes"]
@@ -135,6 +136,7 @@ def lib():
         L.grid_verify_workspace_bytes.argtypes = [i32, i32, i32]
         L.grid_verify_workspace_bytes.restype = sz
         L.grid_tree_masks.argtypes = [vp, vp]
+        L.grid_tree_masks_window.argtypes = [vp, i32, vp]
         L.grid_kv_append_tree.argtypes = [vp, vp, vp, vp, vp]
         L.grid_attend_tree.argtypes = [vp, vp, vp, vp, vp]
         L.grid_attend_tree_workspace_bytes.argtypes = [vp, vp, vp]

@@ -85,21 +85,23 @@ def sample(logits, *, mask=None, temperature=None, top_k=None, top_p=None, min_p
     return _done(_step.sample(logits, mask, temperature, top_k, top_p, min_p, noise, tokens, logprobs, workspace))
 
 
-def tree_masks(parent, cu_q, max_q, *, masks=None, depth=None, stream=None):
+def tree_masks(parent, cu_q, max_q, *, window=0, masks=None, depth=None, stream=None):
     """grid_tree_masks: of every node of the chunks' trees (parent int32 [tokens]: the place of a node's parent in its
-    chunk, before its own; -1: none) the places of itself and its ancestors as bits, and its depth.  Returns (masks int32
-    [tokens, ceil(max_q / 32)], depth int32 [tokens])."""
+    chunk, before its own; -1: none) the places of itself and its ancestors as bits, and its depth.  With a window only the
+    nearest ancestors have bits, `window` places with the node itself: attend_tree under a window asks for such masks where
+    trees may be deeper than it.  Returns (masks int32 [tokens, ceil(max_q / 32)], depth int32 [tokens])."""
     if stream is not None:
         with torch.cuda.stream(stream):
-            return tree_masks(parent, cu_q, max_q, masks=masks, depth=depth)
-    return _done(_step.tree_masks(parent, cu_q, max_q, masks, depth))
+            return tree_masks(parent, cu_q, max_q, window=window, masks=masks, depth=depth)
+    return _done(_step.tree_masks(parent, cu_q, max_q, masks, depth, window))
 
 
 def attend_tree(q, k_pages, v_pages, block_table, kv_len, cu_q, tree, max_q, max_kv, *, depth=None, scale=None, window=0,
                 out=None, lse=None, workspace=None, stream=None):
     """grid_attend_tree: attend for chunks that are trees.  A token sees what is cached before its chunk, and of its chunk
     the places whose bits are set in its row of tree (int32 [tokens, words], as tree_masks writes them).  With a window
-    depth (int32 [tokens]) says where the tokens are.  Returns (out like q, lse float32 [tokens, heads])."""
+    depth (int32 [tokens]) says where the tokens are; it bounds what is cached before the chunk, the bits the chunk itself
+    (tree_masks with the same window).  Returns (out like q, lse float32 [tokens, heads])."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return attend_tree(q, k_pages, v_pages, block_table, kv_len, cu_q, tree, max_q, max_kv, depth=depth,
