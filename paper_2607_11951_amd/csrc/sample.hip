@@ -1010,7 +1010,9 @@ __global__ __launch_bounds__(kThreads, 6) void draw_kernel(SampleArgs a) {
       else
         mass = x.by_digits(best, l_listed);
       if (tid > 0) return;
-      z += (float)((double)mass * __builtin_ldexp(1.0, -x.shift)) * __builtin_amdgcn_exp2f(__builtin_fmaf(-m, r.c, x.edge()));
+      // (where nothing is listed the edge may be out of all bounds)
+      if (mass)
+        z += (float)((double)mass * __builtin_ldexp(1.0, -x.shift)) * __builtin_amdgcn_exp2f(__builtin_fmaf(-m, r.c, x.edge()));
       if (best > first)
         write_token(a, r, b, best, l_listed, m, z);
       else

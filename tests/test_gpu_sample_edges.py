@@ -53,3 +53,13 @@ def test_large_vocabularies_under_a_mask(G):  # noqa: F811
     check(x, G)
     x = Rows(1, 1 << 20, "bf16", seed=4, share=0.4, std=0.0, p=[0.9])
     check(x, G)
+
+
+@pytest.mark.parametrize("temp", [1e-8, 1e-10, 1e-20, 1e-30])
+@pytest.mark.parametrize("shift", [0.0, 20.0, -300.0, 1e4])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_min_p_alone_at_low_temperatures(G, temp, shift, dtype):  # noqa: F811
+    """scaled logits far outside of what a bin's number or a float's unit tells apart"""
+    x = Rows(6, 9000, dtype, seed=21, temps=[temp], q=[0.05, 0.5, 0.9])
+    x.logits = (x.logits.float() + shift).to(DT[dtype])
+    check(x, G)
