@@ -67,7 +67,7 @@ __device__ int status_of(const Paged& P, const AppendArgs& a, int b, bool ordere
       lo = lane == i ? lo : own_lo;
       hi = lane == i ? hi : own_hi;
     }
-    ok = ok && lo >= 0 && (!a.cos || (int64_t)c.kv - c.n + hi < a.n_positions);
+    ok = ok && lo >= 0 && (!a.cos || c.n == 0 || (int64_t)c.kv - c.n + hi < a.n_positions);
   }
   if (ok && c.n > 0) {
     const uint32_t from = P.page.quot((uint32_t)(c.kv - c.n)), to = P.page.quot((uint32_t)(c.kv - 1));
