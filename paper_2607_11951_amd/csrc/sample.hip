@@ -856,8 +856,12 @@ __global__ __launch_bounds__(kThreads, 6) void draw_kernel(SampleArgs a) {
       const Piece y = a.piece[b * a.pieces + p];
       const float f = y.m > -INFINITY ? __builtin_amdgcn_exp2f((y.m - m) * r.c) : 0.f;
       z += y.z * f;
-      const float score = r.greedy ? (y.m == m ? 1.f : 0.f) : __uint_as_float((uint32_t)(y.best >> 32)) * f;
-      const uint64_t key = y.best ? race_key(score, (int)~(uint32_t)y.best) : 0;
+      // A piece's best runs again relative to the row's largest logit: equals of different pieces stay equal, which scores of
+      // the pieces times their factors would not be in the last bit.
+      const int t = (int)~(uint32_t)y.best;
+      float score = y.m == m ? 1.f : 0.f;
+      if (!r.greedy && y.best) score = __builtin_amdgcn_exp2f((y.l - m) * r.c) * __builtin_amdgcn_rcpf(r.noise[t]);
+      const uint64_t key = y.best ? race_key(score, t) : 0;
       l = key > best ? y.l : l;
       best = max(best, key);
     }

@@ -63,3 +63,22 @@ def test_min_p_alone_at_low_temperatures(G, temp, shift, dtype):  # noqa: F811
     x = Rows(6, 9000, dtype, seed=21, temps=[temp], q=[0.05, 0.5, 0.9])
     x.logits = (x.logits.float() + shift).to(DT[dtype])
     check(x, G)
+
+
+@pytest.mark.parametrize("filters", [{}, {"q": [1e-4]}, {"k": [30000]}])
+def test_equals_in_different_pieces(G, filters):  # noqa: F811
+    """equal logits with equal noise, below other largest logits all over the row: the lowest index"""
+    B, V = 64, 45000
+    x = Rows(B, V, "f32", seed=22, temps=[1.0, 0.7, 1.9], **filters)
+    r = np.random.default_rng(5)
+    x.logits = torch.full((B, V), -9.0)
+    x.noise[:] = 1.0
+    first = []
+    for b in range(B):
+        tops, equals = r.choice(V, 40, replace=False), np.sort(r.choice(V, 30, replace=False))
+        x.logits[b, tops] = torch.from_numpy(r.uniform(0.1, 3.0, 40).astype(np.float32))
+        x.noise[b, tops] = 1e6
+        x.logits[b, equals] = float(r.uniform(-0.5, 0.0))
+        x.noise[b, equals] = 1e-3
+        first.append(int(equals[0]))
+    assert x.run(G)[0].tolist() == first
