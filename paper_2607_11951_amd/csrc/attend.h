@@ -650,7 +650,7 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void tiles_kernel(Paged P
   const uint32_t per = (uint32_t)(a.tiles * a.splits);
   uint32_t id = 0, rank = 0;
   int split = 0, tile, g, b;
-  if (a.bundle == kPacked) {
+  if (!X::TREE && a.bundle == kPacked) {
     // Many sequences of which few have many rows: workgroups are numbered by the rows there are.  The tiles of sequence b are
     // numbers cu_q[b] * group / TM + b (rounded down) and on; for a chunk of n tokens the next sequence's begin n * group / TM,
     // rounded down, and 1 later at least, so after its last.  The sequence is the last whose numbers begin at or before this one.
@@ -690,7 +690,7 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void tiles_kernel(Paged P
     rank = in / side;
     id = first + in - rank * side;
   }
-  if (a.bundle != kPacked) {
+  if (X::TREE || a.bundle != kPacked) {
     split = (int)(rank / (uint32_t)a.tiles);
     tile = a.tiles - 1 - (int)(rank % (uint32_t)a.tiles);
     g = (int)(id % (uint32_t)P.hkv);
@@ -700,7 +700,7 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void tiles_kernel(Paged P
   // Whether the chunks before are in order is asked now and told when the pages have been looked up: up to 1000 sequences
   // that costs nothing that shows (chunks of 9 tokens after 300, 16 heads on 2 of 64: 60 sequences 9.6 us, 1000 64.0, and 62.9
   // without), 4000 take 223 us and 216 without, 16000 846 and 735.
-  const bool searched = a.bundle == kPacked;  // they were looked at above
+  const bool searched = !X::TREE && a.bundle == kPacked;  // they were looked at above
   const OrderBefore before(P, b, (int)threadIdx.x);
   if (is_bad(a, ch)) {
     if (split > 0 || tile > 0 || g > 0) return;
@@ -901,9 +901,11 @@ __global__ __launch_bounds__(X::NT, X::W * X::WGS / 4) void shares_kernel(Paged 
   }
 }
 
-// The parts of a row (a token and head) joined by WAVES waves: D / 4 lanes a part, several parts side by side.
+// The parts of a row (a token and head) joined by WAVES waves: D / 4 lanes a part, several parts side by side.  Trees have parts
+// of shares only.
 template <typename T, int D, int TM, bool SHARES, int WAVES, bool TREE>
 __global__ __launch_bounds__(256) void join_kernel(Paged P, AttendArgs a) {
+  static_assert(SHARES || !TREE, "");
   constexpr int L = D / 4, N = 64 * WAVES / L, R = 4 / WAVES;  // lanes a part, parts side by side, rows a workgroup
   const int tid = (int)threadIdx.x, lane = tid & 63, in = tid % (64 * WAVES), e = in % L * 4, side = in / L;
   const uint32_t u = blockIdx.x * R + (uint32_t)tid / (64 * WAVES);
@@ -922,11 +924,10 @@ __global__ __launch_bounds__(256) void join_kernel(Paged P, AttendArgs a) {
       to = run.y;
       live = from != to;
     } else {
-      // the first and the last position that the tile's rows see (or more)
-      const int start = first_key(a, ch), first = ch.kv - ch.n, low = TREE ? first : first + t - ch.first;
+      const int start = first_key(a, ch), pos = ch.kv - ch.n + t - ch.first;
       live = ch.kv - start > a.len;
-      from = (max(a.window ? low - a.window + 1 : 0, start) - start) / a.len;
-      to = ((TREE ? ch.kv - 1 : low) - start) / a.len;
+      from = (max(a.window ? pos - a.window + 1 : 0, start) - start) / a.len;
+      to = (pos - start) / a.len;
       slots = (((int64_t)b * P.hkv + g) * a.tiles + r / TM) * a.splits;
     }
   }
@@ -1079,7 +1080,7 @@ Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_atten
   }
   s.blocks = heads * s.tiles;
   // a joining workgroup a row has to fit a launch
-  if (s.tm == 128 && 4 * s.blocks < 3 * s.at_once && (int64_t)x->n_tokens * g->n_heads <= 1 << 22) {
+  if (!tree && s.tm == 128 && 4 * s.blocks < 3 * s.at_once && (int64_t)x->n_tokens * g->n_heads <= 1 << 22) {
     const int64_t len = (std::max<int64_t>(512, span * s.blocks / (4 * kComputeUnits)) + 127) / 128 * 128;
     if (len < span) {  // ranges alike
       s.splits = (int)((span + len - 1) / len);
@@ -1087,7 +1088,7 @@ Shape shape_of(const grid_paged_cache* c, const grid_chunks* x, const grid_atten
       s.blocks *= s.splits;
     }
   }
-  if (s.blocks > kMostBlocks) {
+  if (!tree && s.blocks > kMostBlocks) {  // (trees are taken whole only where they fit a launch)
     s.packed = true;
     s.blocks = c->n_kv_heads * ((int64_t)x->n_tokens * group / s.tm + x->n_seqs);
   }
@@ -1118,12 +1119,14 @@ void launch(const Paged& P, const AttendArgs& a, const Shape& s, hipStream_t str
     go(Tile<T, D, RW, KW, KT, WGS, true, TREE>());
   else
     go(Tile<T, D, RW, KW, KT, WGS, false, TREE>());
-  if (!s.join) return;
-  const unsigned rows = (unsigned)P.T * (unsigned)a.hq;
-  if (s.parts <= 16)  // a row's: a wave takes them in a few steps
-    hipLaunchKernelGGL((join_kernel<T, D, RW * 32, SHARES, 1, TREE>), dim3((rows + 3) / 4), dim3(256), 0, stream, P, a);
-  else
-    hipLaunchKernelGGL((join_kernel<T, D, RW * 32, SHARES, 4, TREE>), dim3(rows), dim3(256), 0, stream, P, a);
+  if constexpr (SHARES || !TREE) {
+    if (!s.join) return;
+    const unsigned rows = (unsigned)P.T * (unsigned)a.hq;
+    if (s.parts <= 16)  // a row's: a wave takes them in a few steps
+      hipLaunchKernelGGL((join_kernel<T, D, RW * 32, SHARES, 1, TREE>), dim3((rows + 3) / 4), dim3(256), 0, stream, P, a);
+    else
+      hipLaunchKernelGGL((join_kernel<T, D, RW * 32, SHARES, 4, TREE>), dim3(rows), dim3(256), 0, stream, P, a);
+  }
 }
 
 // Waves of rows and of keys, keys a wave and workgroups a compute unit, by what fits in LDS and registers.
