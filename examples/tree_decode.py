@@ -30,6 +30,7 @@ from draft_decode import CAP, Model, tokenize  # noqa: E402
 from workloads import make_workload  # noqa: E402
 
 PAGE = 16
+NODES = 1024  # of a tree, at most; longer prompts go through the model in such pieces
 OFFSET = G.CONFIG_DTYPE.fields["stk_off"][1] // 4  # of a configuration's words: where its stack begins
 
 
@@ -153,7 +154,9 @@ def decode(model, wl, rows=4, samples=2, new_tokens=40, branches=3, depth=4, tem
     # the prompts, but for their last tokens, once; then the continuations from them
     head = [p[:-1] or p for p in prompts]
     cache.go_on([-1] * R, [0] * R, [len(p) for p in head])
-    run(head, [list(range(-1, len(p) - 1)) for p in head], [0] * R)
+    for at in range(0, max(map(len, head)), NODES):
+        piece = [p[at:at + NODES] for p in head]
+        run(piece, [list(range(-1, len(p) - 1)) for p in piece], [min(at, len(p)) for p in head])
     start = [len(p) - 1 for p in prompts]
     cache.go_on(of, [start[r] for r in of], [start[r] for r in of])
     gen = torch.Generator(device=device).manual_seed(seed)
