@@ -738,8 +738,10 @@ size_t grid_verify_workspace_bytes(int32_t B, int32_t K, int32_t V);
  * 32) says that place j of t's chunk is t or an ancestor of t; depth[t] as
  * above.  Bits past the chunk are 0.  Rows of sequences whose chunk is not in
  * order, or longer than max_q, are zero bits and depth 0; rows of tokens that
- * belong to no sequence are left as they are.  stride_words >= ceil(max_q /
- * 32); n_tokens, n_seqs and cu_q as in grid_chunks. */
+ * belong to no sequence are left as they are, and so are words past
+ * ceil(max_q / 32) <= stride_words; n_tokens, n_seqs and cu_q as in grid_chunks.
+ * A prompt of more tokens than a tree has places goes in pieces, or is no tree
+ * but a chunk (grid_kv_append, grid_attend). */
 typedef struct {
   int32_t n_seqs;
   int32_t n_tokens;
@@ -761,7 +763,7 @@ int grid_tree_masks_window(const grid_tree_args* args, int32_t window, void* str
 /* grid_kv_append for trees: keys and queries are rotated by the position first
  * + depth[t] (first: the cached tokens before the chunk), and lie at first +
  * their place in the chunk.  A token of negative depth, or whose position has
- * no row of cos and sin, is left out; so is, in a bad status, its sequence. */
+ * no row of cos and sin, is left out, and its sequence's status is bad. */
 int grid_kv_append_tree(const grid_paged_cache* cache, const grid_chunks* chunks, const grid_append_args* args,
                         const int32_t* depth, void* stream);
 
@@ -797,7 +799,8 @@ size_t grid_attend_tree_workspace_bytes(const grid_paged_cache* cache, const gri
  * Of a bad sequence, an empty chunk, one longer than max_q, and a start that is
  * not a place in the chunk, length is 0 and next -1, and nothing is moved; nor
  * is a row whose page, or that of its place, is not in the cache.  No page may be
- * in two sequences' chunks. */
+ * in two sequences' chunks.  GRID_E_CAPACITY where n_seqs * n_layers *
+ * ceil(n_kv_heads * head_dim / 1024) is more than 2^23. */
 typedef struct {
   const int32_t* tokens;       /* device [n_tokens]: the drafted tokens */
   const int32_t* parent;       /* device [n_tokens] */
@@ -819,7 +822,8 @@ int grid_commit_tree(const grid_paged_cache* cache, const grid_chunks* chunks, c
  * 0 .. page_size) of page src[i] to page dst[i], keys and values, in every
  * layer (layer strides as in grid_commit_args).  Pairs with an id that is not
  * in 0 .. n_pages - 1 are left out (-1: none).  No page that is written may be
- * in another pair; a pair of one page twice does nothing. */
+ * in another pair; a pair of one page twice does nothing.  GRID_E_CAPACITY for
+ * pages of 2^33 entries and more. */
 typedef struct {
   const int32_t* src;          /* device [n] */
   const int32_t* dst;          /* device [n] */
@@ -856,7 +860,9 @@ int grid_kv_copy(const grid_paged_cache* cache, const grid_copy_args* args, void
  * copy) when parent is less than -1 or not below n_in, keep is negative or more
  * than its parent's pages, room's pages are more than table_cols, or one of the
  * entries it keeps is not a page.  held is clamped to 0 .. table_cols; entries
- * that are not pages are not counted.  Without a parent keep is 0.
+ * that are not pages are not counted.  Without a parent keep is 0.  Every row looks
+ * at the rows before it: the work grows with n_rows squared, which shows from some
+ * ten thousand rows on.
  * refs_out may be refs.  No two of the other arrays may overlap. */
 typedef struct {
   const int32_t* table;        /* device [n_in][table_stride] */
@@ -900,8 +906,9 @@ size_t grid_kv_fork_workspace_bytes(int32_t n_rows, int32_t n_pages);
  * logit, its log p at temperature 1 among all allowed tokens, no filters.
  * A row with no distribution (nothing allowed, or an allowed logit that is NaN or
  * +inf) gives the token -1 and 0; so does one where noise that is not finite
- * leaves no kept token a p / noise above 0 (noise is above 0 and finite; it has
- * a part at kept tokens only).  top_p or min_p that is NaN keeps all.  Where
+ * leaves no kept token a p / noise above 0 (noise is from 2^-126 to 2^126; it is
+ * read, and has a part, at kept tokens only, but all of a row's V are in place:
+ * drawing them is the caller's).  top_p or min_p that is NaN keeps all.  Where
  * top_k or top_p are in force a p below 2^-60 of the largest counts as 0.
  * Statistics are held in 32 bits or more. */
 typedef struct {

@@ -11,6 +11,8 @@
 // whether its last page has to be copied and how many pages it needs, and which pages are free, 64 a word; the fourth gives
 // the rows theirs: a row's first is as many free pages on as the rows before it need.  Forks are bound by reads that wait for
 // others and the borders between launches: 512 rows of up to 8192 tokens, pages of 16, take 19.2 us (4.1, 5.1, 3.4 and 7.2 a launch).
+// Every row adds up the needs of those before it, and one that shares its last page looks at all rows' last pages: 4096 rows
+// that grow take 31 us and forked in pairs 46, 16384 109 and 228, 65535 732 and 1960.
 #include <algorithm>
 #include <string>
 

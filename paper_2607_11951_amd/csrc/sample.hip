@@ -18,7 +18,7 @@
 // are 14, a workgroup's vector units being busy half of the time; then noise and what a flat nucleus lists, ordered by
 // digits.  32 rows of 151936 in bf16 take 11 and 18 us, one 6 and 12: some ten dependent reads in two launches, and the
 // pieces' histograms, which every workgroup of a row adds up for itself (a launch that did it once would cost what it
-// saves).  A workgroup remembers each wave's largest logit of a step, so waves whose tokens are all below the cuts do not read
+// saves; it grows with the square of V: a row of 4 million 58 us, 16 million 388, 64 million 4.6 ms).  A workgroup remembers each wave's largest logit of a step, so waves whose tokens are all below the cuts do not read
 // them again: of the 256 rows 54 us for 65.
 #include <algorithm>
 #include <string>
@@ -533,7 +533,9 @@ __device__ inline Bins bins_of(const SampleArgs& a, const Row& r, int64_t b, flo
         const float part = __builtin_amdgcn_exp2f(-(float)(off % kPerOctave) * (1.f / kPerOctave));
         all += (uint64_t)((double)x.best * __builtin_ldexp((double)part, -(off / kPerOctave)));
       }
-      constexpr int kAhead = 10;  // pieces that are asked for together
+      // Pieces that are asked for together.  It matters little: of 32000 to 262144 tokens, 1 to 256 rows, top_k 50 or a nucleus
+      // of 0.9, passes take with 4, 8 and 16 between 3 % less and 3 % more than with 10, with 20 up to 6 % more.
+      constexpr int kAhead = 10;
       for (int p = 0; p < min(64, a.pieces - p0); p += kAhead) {
         uint64_t y[kAhead];
 #pragma unroll

@@ -6,7 +6,7 @@
 // child, the lowest place counts, and the path is followed; every workgroup of a sequence does so for itself, and moves
 // its columns of the rows: a thread has the same 16 bytes of all rows, so those it writes are those it has read before.
 //
-// The masks are bound by a handful of dependent reads (32 trees of 64 nodes 4 us, one of 1024, a chain, 21; followed place by
+// The masks are bound by a handful of dependent reads (32 trees of 64 nodes 3.4 us, one of 1024, a chain, 22; followed place by
 // place 134), and so is the commit of few sequences (a chain of 64 nodes, all kept, 7 us; with a search of the chunk a node 20).
 // 64 trees of up to 64 nodes, 8 heads of 128 in 32 layers, take 14 us: 5 until the branches are known, then their bytes (with
 // rows that the caches keep, which nobody reads soon, 5 more).

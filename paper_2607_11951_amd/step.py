@@ -76,7 +76,8 @@ def sample(logits, *, mask=None, temperature=None, top_k=None, top_p=None, min_p
     """grid_sample: one token of every row of logits [B, V] under the mask rows (int32 [B, words], as Grid.mask writes them;
     None: all tokens allowed), at the rows' temperature (float32 [B]), of the top_k (int32 [B]) largest, of these the ones
     that hold top_p (float32 [B]) of the mass, of these the ones with at least min_p (float32 [B]) of the largest
-    probability.  noise (float32 [B, V], from Exp(1)) are the random numbers; without them the token is the largest logit's.
+    probability.  noise (float32 [B, V], from Exp(1)) are the random numbers, drawn by the caller for all V whatever is kept;
+    without them the token is the largest logit's.
     Returns (tokens int32 [B], -1 where there is none; logprobs float32 [B], of the token among those that are kept)."""
     if stream is not None:
         with torch.cuda.stream(stream):
@@ -87,8 +88,8 @@ def sample(logits, *, mask=None, temperature=None, top_k=None, top_p=None, min_p
 
 def tree_masks(parent, cu_q, max_q, *, window=0, masks=None, depth=None, stream=None):
     """grid_tree_masks: of every node of the chunks' trees (parent int32 [tokens]: the place of a node's parent in its
-    chunk, before its own; -1: none) the places of itself and its ancestors as bits, and its depth.  With a window only the
-    nearest ancestors have bits, `window` places with the node itself: attend_tree under a window asks for such masks where
+    chunk, before its own; -1: none) the places of itself and its ancestors as bits, and its depth.  A chunk has max_q places at
+    most, max_q is at most 1024.  With a window only the nearest ancestors have bits, `window` places with the node itself: attend_tree under a window asks for such masks where
     trees may be deeper than it.  Returns (masks int32 [tokens, ceil(max_q / 32)], depth int32 [tokens])."""
     if stream is not None:
         with torch.cuda.stream(stream):
