@@ -18,8 +18,9 @@
 // are 14, a workgroup's vector units being busy half of the time; then noise and what a flat nucleus lists, ordered by
 // digits.  32 rows of 151936 in bf16 take 11 and 18 us, one 6 and 12: some ten dependent reads in two launches, and the
 // pieces' histograms, which every workgroup of a row adds up for itself (a launch that did it once would cost what it
-// saves; it grows with the square of V: a row of 4 million 58 us, 16 million 388, 64 million 4.6 ms).  A workgroup remembers each wave's largest logit of a step, so waves whose tokens are all below the cuts do not read
-// them again: of the 256 rows 54 us for 65.
+// saves; it grows with the square of V: a row of 4 million 58 us, 16 million 388, 64 million 4.6 ms).  A workgroup remembers
+// each wave's largest logit of a step, so waves whose tokens are all below the cuts do not read them again: of the 256 rows
+// 54 us for 65.
 #include <algorithm>
 #include <string>
 #include <type_traits>

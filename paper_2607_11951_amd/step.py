@@ -88,9 +88,9 @@ def sample(logits, *, mask=None, temperature=None, top_k=None, top_p=None, min_p
 
 def tree_masks(parent, cu_q, max_q, *, window=0, masks=None, depth=None, stream=None):
     """grid_tree_masks: of every node of the chunks' trees (parent int32 [tokens]: the place of a node's parent in its
-    chunk, before its own; -1: none) the places of itself and its ancestors as bits, and its depth.  A chunk has max_q places at
-    most, max_q is at most 1024.  With a window only the nearest ancestors have bits, `window` places with the node itself: attend_tree under a window asks for such masks where
-    trees may be deeper than it.  Returns (masks int32 [tokens, ceil(max_q / 32)], depth int32 [tokens])."""
+    chunk, before its own; -1: none) the places of itself and its ancestors as bits, and its depth.  A chunk has max_q places
+    at most, max_q is at most 1024.  With a window only the nearest ancestors have bits, `window` places with the node
+    itself: attend_tree under a window asks for such masks where trees may be deeper than it.  Returns (masks int32 [tokens, ceil(max_q / 32)], depth int32 [tokens])."""
     if stream is not None:
         with torch.cuda.stream(stream):
             return tree_masks(parent, cu_q, max_q, window=window, masks=masks, depth=depth)
